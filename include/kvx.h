@@ -40,7 +40,12 @@ enum kv_status {
   KV_E_HIP = -5      /* a HIP runtime call failed                         */
 };
 
-enum kv_dtype { KV_BF16 = 0, KV_F32 = 1 };
+enum kv_dtype {
+  KV_BF16 = 0,
+  KV_F32 = 1,
+  KV_F16 = 2,  /* paged cache only (kv_paged_config)                                              */
+  KV_E4M3 = 3  /* paged cache only, as its cache_dtype: 8 bits, 4 exponent and 3 mantissa bits     */
+};
 
 enum kv_meta_format {
   KV_META_F32 = 0,  /* per group an fp32 scale and an int32 zero-point (8 bytes): the stored values are    */
@@ -327,6 +332,154 @@ int kv_set_option(kv_handle* h, const char* name, int64_t value);
  * Both return KV_OK or a negative kv_status. */
 int kv_probe_mfma_bf16(int32_t iters, int32_t repeats, void* hip_stream, double* tflops);
 int kv_probe_copy(int64_t bytes, int32_t repeats, void* hip_stream, double* gbytes_per_s);
+
+/* ---- paged cache -----------------------------------------------------------------------------------------
+ *
+ * The caches above belong to a handle and hold frames of one size.  The calls below work on a pool of pages that the
+ * caller owns and that sequences of uneven lengths share: a sequence's j-th cached token lies in slot j % page_size of
+ * page page_table[sequence][j / page_size].  Query heads may share key heads (n_q_heads a multiple of n_kv_heads: query
+ * head g reads key head g / (n_q_heads / n_kv_heads)).  One step of a layer is
+ *   kv_paged_append   rotary positions for the new tokens' queries and keys, keys and values into the pages
+ *   kv_paged_attend   attention of the new tokens over their sequences' pages (one new token each: decoding), and the
+ *                     weights that the cached tokens receive in it
+ *   kv_paged_evict    sequences over a budget give up the tokens that received the least
+ *
+ * Everything a call needs of the sequences' state (page table, lengths, where each sequence's new tokens begin) is read
+ * on the device when the call's kernels run, so a captured call replays on whatever these arrays hold then; the host
+ * gives upper bounds.  No call allocates, synchronises or copies; work is enqueued on hip_stream.  A handle owns the
+ * rotary frequencies and a workspace (partial results), nothing of the sequences: calls on one handle, replays of
+ * captured ones included, must be stream-ordered with each other, and callers that want two at once use two handles.
+ * The device that was current at kv_paged_init has to be current in every call (KV_E_STATE otherwise) and to hold every
+ * device pointer.
+ *
+ * Lengths and page numbers are the device's to read, so no call can refuse them; kernels stay inside what the host gave
+ * all the same: a page outside [0, n_pages) holds no tokens (attend sees none of its slots, append drops what belongs
+ * there, evict lets its tokens go first), lengths and offsets are cut to [0, max_len], [0, max_new] and [0, n_tokens].
+ * kv_paged_status tells whether that happened. */
+
+enum kv_rope_layout {
+  KV_ROPE_HALF = 0,        /* channel i of a head turns with channel i + rotary_dim / 2             */
+  KV_ROPE_INTERLEAVED = 1  /* channel 2 i turns with channel 2 i + 1                                */
+};
+
+enum kv_rope_scaling {     /* w_i = rope_base ^ (-2 i / rotary_dim) radians per position, i < rotary_dim / 2 */
+  KV_ROPE_PLAIN = 0,       /* w_i                                                                    */
+  KV_ROPE_LINEAR = 1,      /* w_i / factor                                                           */
+  KV_ROPE_BASE = 2,        /* the base is rope_base * factor ^ (rotary_dim / (rotary_dim - 2))       */
+  KV_ROPE_PARTS = 3        /* t_i = rope_original_len * w_i / 2 pi turns over the original length; w_i where  */
+                           /* t_i >= rope_high_turns, w_i / factor where t_i <= rope_low_turns, between them  */
+                           /* the mean of the two weighted linearly in t_i                                    */
+};
+
+typedef struct kv_paged_config {
+  int32_t n_q_heads;       /* Hq, 1..1024, a multiple of n_kv_heads                                */
+  int32_t n_kv_heads;      /* Hkv, 1..256; Hq / Hkv at most 128                                    */
+  int32_t head_dim;        /* d: 64 or 128                                                         */
+  int32_t page_size;       /* slots of a page: a power of two, 8..1024                             */
+  int32_t dtype;           /* of q, k, v and out: KV_BF16 or KV_F16                                */
+  int32_t cache_dtype;     /* of the pages: the same, or KV_E4M3                                   */
+  int32_t max_seqs;        /* most sequences of a call, 1..65536                                   */
+  int32_t max_tokens;      /* most new tokens of a call, 1..2^22                                   */
+  int32_t max_len;         /* most cached tokens of a sequence, 1..2^27                            */
+  int32_t max_evicted;     /* most tokens of one sequence that kv_paged_evict has to move, 0 -> max_len / 2; */
+                           /* 8 bytes of workspace for each, sequence and key head                  */
+  float softmax_scale;     /* 0 -> 1/sqrt(head_dim)                                                */
+  int32_t rotary_dim;      /* first channels of a head that turn: a multiple of 16 up to d; 0: none */
+  int32_t rope_layout;     /* kv_rope_layout                                                       */
+  int32_t rope_scaling;    /* kv_rope_scaling                                                      */
+  int32_t rope_original_len; /* KV_ROPE_PARTS: the length the frequencies were made for            */
+  double rope_base;        /* 0 -> 10000                                                           */
+  double rope_factor;      /* 0 -> 1                                                               */
+  double rope_low_turns;   /* 0 -> 1                                                               */
+  double rope_high_turns;  /* 0 -> 4                                                               */
+  float rope_magnitude;    /* 0 -> 1: what the turned channels are multiplied by                   */
+  const double* rope_freqs; /* host, [rotary_dim / 2] radians per position, read by kv_paged_init; NULL: the   */
+                           /* frequencies above, otherwise these and rope_scaling is not looked at  */
+} kv_paged_config;
+
+typedef struct kv_paged kv_paged;
+
+/* Rows of tokens: device (not looked at where the call has n_tokens = 0); element (token, head, channel) at token * tok_stride + head * head_stride + channel
+ * (strides in elements, every row 16-byte aligned). */
+typedef struct kv_rows {
+  void* data;
+  int64_t tok_stride;
+  int64_t head_stride;
+} kv_rows;
+
+/* The pool and the sequences' places in it.  Strides are in elements of cache_dtype, the same for keys and values;
+ * element (page, slot, head, channel) at page * page_stride + slot * slot_stride + head * head_stride + channel, so both
+ * orders of slots and heads are possible; rows of d channels contiguous and 16-byte aligned. */
+typedef struct kv_pages {
+  void* k;                  /* device                                                              */
+  void* v;                  /* device                                                              */
+  int64_t page_stride, slot_stride, head_stride;
+  int32_t n_pages;
+  int32_t pages_per_seq;    /* entries of a page table row                                         */
+  const int32_t* page_table; /* device, [n_seqs][pages_per_seq], rows table_stride apart           */
+  int64_t table_stride;
+  const float* k_scale;     /* device, [Hkv], KV_E4M3: a stored key times its head's scale is the  */
+  const float* v_scale;     /* key (values likewise); NULL: 1.  Positive and finite                */
+  float* weights;           /* device, [n_pages][Hkv][page_size]: weight each cached token has received; NULL: not kept */
+  int32_t* ids;             /* device, [n_pages][Hkv][page_size]: which token of its sequence a slot holds; NULL: not kept */
+} kv_pages;
+
+/* The sequences of a call and their new tokens: rows q_start[s] .. q_start[s + 1] - 1 of the call's tensors are the
+ * last tokens of sequence s, whose cached length with them is kv_lens[s].  Rows of no sequence are left alone. */
+typedef struct kv_paged_batch {
+  int32_t n_seqs;
+  int32_t n_tokens;         /* rows of the call's tensors                                          */
+  int32_t max_new;          /* no sequence has more new tokens                                     */
+  int32_t max_len;          /* no sequence is longer                                               */
+  const int32_t* q_start;   /* device, [n_seqs + 1], ascending                                     */
+  const int32_t* kv_lens;   /* device, [n_seqs]                                                    */
+  const int32_t* seen;      /* device, [n_seqs]: tokens the sequence has had in all, evicted ones included; NULL: kv_lens */
+} kv_paged_batch;
+
+/* Check the configuration, allocate the workspace and the rotary frequencies.  cfg: host. out: host, receives the handle. */
+int kv_paged_init(const kv_paged_config* cfg, kv_paged** out);
+
+/* New tokens into the cache.  Queries and keys turn by their positions: angle_i = position * w_i, kept exact for every
+ * int32 position by a 64-bit phase; channels from rotary_dim on pass as they are.  The turned queries go to q_out (which
+ * may be q itself), the turned keys and the values to the pages, for KV_E4M3 divided by the head's scale, rounded to
+ * nearest even and kept within +-448.  Where the pool keeps ids, a new token's is seen - new + its row; where it keeps
+ * weights, its weight starts at 0.  positions: device, [n_tokens]; NULL: the ids.  q and q_out: NULL, both, to leave the
+ * queries out.  A slot that two new tokens name receives either. */
+int kv_paged_append(kv_paged* h, const kv_pages* pages, const kv_paged_batch* batch, const int32_t* positions, const kv_rows* q,
+                    const kv_rows* q_out, const kv_rows* k, const kv_rows* v, void* hip_stream);
+
+/* Attention of the new tokens over their sequences' cached ones, themselves included (kv_paged_append comes first).  The
+ * token of row i of a sequence with `new` rows and cached length len has place p = len - new + i and sees the places
+ * 0 <= j < len, with causal != 0 only j <= p, with window > 0 only j > p - window.  out: softmax of softmax_scale q.k over them times
+ * the values, zero where a row sees nothing; keys and values that a row does not see have no part in its result whatever
+ * they hold.  lse: device, [n_tokens][Hq] fp32, natural logarithm of the softmax's sum (-infinity where nothing is
+ * seen); NULL: not wanted.  weights_out: device, laid out as pages->weights; for every cached token of every sequence of the
+ * call and every key head pages->weights plus the softmax weights the token received, summed over the call's rows and the
+ * heads of the group; may be pages->weights itself; other slots are left alone.  NULL: not wanted.  A page may be in
+ * several sequences' tables (a shared prefix), but not with weights_out. */
+int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* batch, const kv_rows* q, const kv_rows* out,
+                    float* lse, int32_t causal, int32_t window, float* weights_out, void* hip_stream);
+
+/* Sequences longer than budget are brought down to it, every key head for itself: tokens with ids below `sinks` and the
+ * `recent` last ones (ids from seen - recent on) stay, of the others those with the largest pages->weights (NaN counts as the
+ * least; of equal ones the lower slot).  (Should more than budget be protected, the lower slots stay.)  Slots below the
+ * budget that lose their token receive, in ascending order, the tokens that stay but lie behind the budget; nothing else
+ * moves, so a cache that gives up one token a step moves one.  weights_out, ids_out (device, laid out as pages->weights,
+ * may be the same) receive what the slots below the new length hold then; lens_out (device, [n_seqs], may be kv_lens)
+ * receives min(kv_lens, budget).  The order of cached tokens is not kept, so a window (above) no longer counts
+ * arrivals.  Pages must not be shared between sequences.  Needs pages->weights and pages->ids; sinks + recent <= budget. */
+int kv_paged_evict(kv_paged* h, const kv_pages* pages, const kv_paged_batch* batch, int32_t budget, int32_t sinks, int32_t recent,
+                   float* weights_out, int32_t* ids_out, int32_t* lens_out, void* hip_stream);
+
+/* What calls since the last kv_paged_status met on the device (host, overwritten): bit 0, a page number outside the pool
+ * in a place that was needed; bit 1, a length or an offset outside what the host gave.  Synchronises the device. */
+int kv_paged_status(kv_paged* h, int32_t* flags);
+
+/* Free everything.  NULL is allowed.  A captured call must not be replayed afterwards. */
+void kv_paged_destroy(kv_paged* h);
+
+/* Text of the last error on this handle (or of the last failed kv_paged_init when h is NULL). */
+const char* kv_paged_last_error(kv_paged* h);
 
 #ifdef __cplusplus
 }

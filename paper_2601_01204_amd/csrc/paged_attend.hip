@@ -1,0 +1,402 @@
+// Attention of new tokens over a paged cache.
+//
+// Rows of one key head (new tokens x heads of the group) are cut into tiles, the keys of a tile into ranges; a workgroup takes one
+// range of one tile.  Tiles of up to 32 rows (decoding) belong to attend_few_kernel, larger ones to attend_chunk_kernel.  With more than
+// one range, workgroups leave partial results and merge_kernel joins them.
+#include "../../include/kvx.h"
+#include "paged_tile.h"
+
+namespace kvx {
+namespace paged {
+
+namespace {
+
+constexpr float kLn2 = 0.69314718055994531f;
+
+// Result of a row: o channels (4 at `ch`), final or partial.
+template <typename T>
+__device__ __forceinline__ void store_out(const AttendArgs& a, int token, int head, int ch, const float (&x)[4]) {
+  *reinterpret_cast<u32x2*>(a.out.p + (int64_t)token * a.out.tok + (int64_t)head * a.out.head + 2 * ch) =
+      (u32x2){T::pack(x[0], x[1]), T::pack(x[2], x[3])};
+}
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
+// ---- up to 32 rows: four waves, each with a ring of units of its own -------------------------------------------
+// Bound by memory: every key and value is read once.  A wave works on every fourth unit of the range, brings it through registers into
+// its own part of LDS and holds the next unit's loads in flight meanwhile (16 KB a wave, 8 waves a compute unit); no wave waits
+// for another before the end, where the four waves' statistics and outputs are joined through the same LDS.
+template <typename T, int D, bool E4M3>
+__global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) {
+  typedef Shape<D, E4M3> S;
+  constexpr int kRB = S::kRowBytes, kLPR = S::kLanesPerRow;
+  constexpr int kLoads = 32 * kLPR / 64;                     // 16-byte loads of a lane for 32 rows
+  constexpr int kWaveBytes = 64 * kRB;
+  constexpr int kJoinBytes = 32 * D * 4;
+  __shared__ __align__(16) uint8_t lds[4 * (kWaveBytes > kJoinBytes ? kWaveBytes : kJoinBytes)];
+  __shared__ float2 stats[4][32];
+
+  const Call& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
+  const int split = rest % a.splits, tile = rest / a.splits;
+  int b, t;
+  if (!find_tile(a, tile, 32, b, t)) return;
+  const Seq s = sequence(c, b);
+  const int rows = s.n * c.group, row0 = t * 32;
+  if (row0 >= rows) return;
+  const int n_rows = min(32, rows - row0);
+  const Range range = tile_range(a, s, row0, n_rows);
+  const int n_splits = splits_of(a, range);
+  if (split >= n_splits) return;
+  const int k0 = range.lo + split * a.split_keys, k1 = split_end(a, range, split);
+
+  RowBlock<T, D, E4M3> w;
+  w.clear();
+  const int row = row0 + min(lane & 31, n_rows - 1);         // lanes without a row repeat the last one's
+  const int i_row = row / c.group, g_row = row - i_row * c.group;
+  const int place = s.len - s.n + i_row;
+  w.hi = a.causal ? min(s.len, place + 1) : s.len;
+  w.lo = a.window > 0 ? place + 1 - a.window : 0;
+  w.load_queries(a.q.p + (int64_t)(s.first + i_row) * a.q.tok + (int64_t)(head * c.group + g_row) * a.q.head, h);
+  // keys [all_lo, all_hi) are seen by every row
+  const int all_hi = a.causal ? min(s.len, s.len - s.n + row0 / c.group + 1) : s.len;
+  const int all_lo = a.window > 0 ? s.len - s.n + (row0 + n_rows - 1) / c.group + 1 - a.window : 0;
+  const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
+
+  uint8_t* const lk = lds + wave * kWaveBytes;
+  uint8_t* const lv = lk + 32 * kRB;
+  const int ld_row = lane / kLPR * kLoads, ld_chunk = lane % kLPR;
+  const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
+  const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
+  u32x4 rk[kLoads], rv[kLoads];
+  uint32_t absent_next = 0;
+  int32_t page = -1;
+  auto fetch_page = [&](int u) { page = u < k1 ? page_of_key(c, b, u + (lane & 31), s.len) : 0; };
+  auto fetch_rows = [&](int u) {                             // needs fetch_page(u)
+    const uint64_t bad = __ballot(page < 0);
+    absent_next = (uint32_t)bad;
+    if (bad && lane == 0) note_bad_page(c);
+    const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      rk[i] = *reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride);
+      rv[i] = *reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride);
+    }
+  };
+
+  int u = k0 + 32 * wave;
+  if (u < k1) {
+    fetch_page(u);
+    fetch_rows(u);
+    fetch_page(u + 128);
+  }
+  for (; u < k1; u += 128) {
+    const uint32_t absent = absent_next;
+    // values behind the end and without a page are zero: a probability of zero times what lies there would not be
+    const bool tail = u + 32 > s.len || absent;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = ld_row + i;
+      if (tail && (u + r >= s.len || ((absent >> r) & 1))) rv[i] = (u32x4){0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(lk + lds_offset<kRB>(r, ld_chunk)) = rk[i];
+      *reinterpret_cast<u32x4*>(lv + lds_offset<kRB>(r, ld_chunk)) = rv[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // this wave's LDS only: its accesses are carried out in order
+    __builtin_amdgcn_wave_barrier();
+    if (u + 128 < k1) {
+      fetch_rows(u + 128);
+      fetch_page(u + 256);
+    }
+    f32x16 x = w.logits(lk, lane);
+    if (u + 32 > all_hi || u < all_lo || absent) w.mask(x, u, absent, h);
+    w.soften(x, factor);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w.l += x[r];
+    // probabilities as a pair of 16-bit values, so that they are not rounded before the output is (the matrix cores have time)
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      u32x4 p, p_low;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = x[8 * st + 2 * e], x1 = x[8 * st + 2 * e + 1];
+        p[e] = T::pack(x0, x1);
+        p_low[e] = T::pack(x0 - T::low(p[e]), x1 - T::high(p[e]));
+      }
+#pragma unroll
+      for (int cb = 0; cb < S::kBlocks; ++cb) {
+        const u32x4 f = w.value_fragment(lv, lane, st, cb);
+        w.o[cb] = T::mfma(f, p, w.o[cb]);
+        w.o[cb] = T::mfma(f, p_low, w.o[cb]);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // join the four waves
+  {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
+    w.l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (h == 0) stats[wave][lane] = make_float2(w.m, w.l);
+  __syncthreads();                                           // (also: no wave reads its K and V any more)
+  float m = -kInf;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = fmaxf(m, stats[i][lane & 31].x);
+  const float mine = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
+  float* const jo = reinterpret_cast<float*>(lds) + wave * 32 * D;
+#pragma unroll
+  for (int cb = 0; cb < S::kBlocks; ++cb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) jo[(lane & 31) * D + ((32 * cb + 8 * g + 4 * h + e) ^ (4 * (lane & 7)))] = w.o[cb][4 * g + e] * mine;
+  __syncthreads();
+  const float v_scale = E4M3 && c.v_scale ? c.v_scale[head] : 1.f;
+  const int64_t block = ((int64_t)tile * c.hkv + head) * a.splits + split;
+  for (int at = threadIdx.x; at < n_rows * (D / 4); at += 256) {
+    const int r = at / (D / 4), ch = at % (D / 4) * 4;
+    float top = -kInf, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, stats[i][r].x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += top == -kInf ? 0.f : stats[i][r].y * __builtin_amdgcn_exp2f(stats[i][r].x - top);
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds) + (i * 32 + r) * D + (ch ^ (4 * (r & 7))));
+      o[0] += x.x;
+      o[1] += x.y;
+      o[2] += x.z;
+      o[3] += x.w;
+    }
+    const int row_r = row0 + r, i_r = row_r / c.group, token = s.first + i_r, qh = head * c.group + row_r - i_r * c.group;
+    if (n_splits == 1) {
+      const float f = sum == 0.f ? 0.f : v_scale / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= f;
+      store_out<T>(a, token, qh, ch, o);
+      if (a.lse && ch == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(top, sum);
+    } else {
+      *reinterpret_cast<float4*>(a.part_o + (block * a.part_rows + r) * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
+      if (ch == 0) a.part_ml[block * a.part_rows + r] = make_float2(top, sum);
+    }
+  }
+}
+
+// ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
+constexpr int kChunkRows = 128;
+
+template <typename T, int D, bool E4M3>
+__global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a) {
+  typedef Shape<D, E4M3> S;
+  constexpr int kRB = S::kRowBytes, kLPR = S::kLanesPerRow;
+  constexpr int kLoads = 64 * kLPR / 256;
+  __shared__ __align__(16) uint8_t lds[2][2][64 * kRB];      // [buffer][K, V]
+
+  const Call& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const int columns = c.hkv * a.splits;
+  const int column = blockIdx.x % columns, tile = a.tiles - 1 - blockIdx.x / columns;      // long causal tiles first
+  const int head = column % c.hkv, split = column / c.hkv;
+  int b, t;
+  if (!find_tile(a, tile, kChunkRows, b, t)) return;
+  const Seq s = sequence(c, b);
+  const int rows = s.n * c.group, row0 = t * kChunkRows;
+  if (row0 >= rows) return;
+  const int n_rows = min(kChunkRows, rows - row0);
+  const Range range = tile_range(a, s, row0, n_rows);
+  const int n_splits = splits_of(a, range);
+  if (split >= n_splits) return;
+  const int k0 = range.lo + split * a.split_keys, k1 = split_end(a, range, split);
+
+  RowBlock<T, D, E4M3> w;
+  w.clear();
+  const int first = row0 + 32 * wave, last = min(first + 31, row0 + n_rows - 1);           // of this wave; first > last: none
+  const int row = min(first + (lane & 31), row0 + n_rows - 1);
+  const int i_row = row / c.group, g_row = row - i_row * c.group;
+  const int place = s.len - s.n + i_row;
+  w.hi = a.causal ? min(s.len, place + 1) : s.len;
+  w.lo = a.window > 0 ? place + 1 - a.window : 0;
+  w.load_queries(a.q.p + (int64_t)(s.first + i_row) * a.q.tok + (int64_t)(head * c.group + g_row) * a.q.head, h);
+  const int place_first = s.len - s.n + first / c.group, place_last = s.len - s.n + last / c.group;
+  const int all_hi = a.causal ? min(s.len, place_first + 1) : s.len, any_hi = first > last ? 0 : (a.causal ? min(s.len, place_last + 1) : s.len);
+  const int all_lo = a.window > 0 ? place_last + 1 - a.window : 0, any_lo = a.window > 0 ? place_first + 1 - a.window : 0;
+  const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
+
+  const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR;
+  const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
+  const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
+  u32x4 rk[kLoads], rv[kLoads];
+  uint64_t absent_loaded = 0;                                // of the tile in the registers
+  int32_t page = 0;
+  auto fetch_page = [&](int u) { page = u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
+  auto fetch_rows = [&](int u) {
+    absent_loaded = __ballot(page < 0);
+    if (absent_loaded && threadIdx.x == 0) note_bad_page(c);
+    const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      rk[i] = *reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride);
+      rv[i] = *reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride);
+    }
+  };
+  auto put_rows = [&](int buf, int u) {
+    const bool tail = u + 64 > s.len || absent_loaded;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = ld_row + i;
+      if (tail && (u + r >= s.len || ((absent_loaded >> r) & 1))) rv[i] = (u32x4){0, 0, 0, 0};
+      *reinterpret_cast<u32x4*>(lds[buf][0] + lds_offset<kRB>(r, ld_chunk)) = rk[i];
+      *reinterpret_cast<u32x4*>(lds[buf][1] + lds_offset<kRB>(r, ld_chunk)) = rv[i];
+    }
+  };
+
+  uint64_t absent = 0;
+  if (k0 < k1) {
+    fetch_page(k0);
+    fetch_rows(k0);
+    fetch_page(k0 + 64);
+    put_rows(0, k0);
+    absent = absent_loaded;
+    if (k0 + 64 < k1) {
+      fetch_rows(k0 + 64);
+      fetch_page(k0 + 128);
+    }
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int u = k0; u < k1; u += 64, buf ^= 1) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int key0 = u + 32 * half;
+      if (key0 < any_hi && key0 + 32 > any_lo) {
+        f32x16 x = w.logits(lds[buf][0] + half * 32 * kRB, lane);
+        const uint32_t missing = (uint32_t)(absent >> (32 * half));
+        if (key0 + 32 > all_hi || key0 < all_lo || missing) w.mask(x, key0, missing, h);
+        w.soften(x, factor);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w.l += x[r];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          u32x4 p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = T::pack(x[8 * st + 2 * e], x[8 * st + 2 * e + 1]);
+#pragma unroll
+          for (int cb = 0; cb < S::kBlocks; ++cb) w.o[cb] = T::mfma(w.value_fragment(lds[buf][1] + half * 32 * kRB, lane, st, cb), p, w.o[cb]);
+        }
+      }
+    }
+    if (u + 64 < k1) {
+      put_rows(buf ^ 1, u + 64);                             // read last in the tile before this one, a barrier ago
+      absent = absent_loaded;
+      if (u + 128 < k1) {
+        fetch_rows(u + 128);
+        fetch_page(u + 192);
+      }
+    }
+    __syncthreads();
+  }
+
+  {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
+    w.l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if (first + (lane & 31) > last) return;
+  const int token = s.first + i_row, qh = head * c.group + g_row;
+  const bool whole = n_splits == 1;
+  const int64_t part_row = (((int64_t)tile * c.hkv + head) * a.splits + split) * a.part_rows + (row - row0);
+  const float f = whole ? (w.l == 0.f ? 0.f : (E4M3 && c.v_scale ? c.v_scale[head] : 1.f) / w.l) : 1.f;
+#pragma unroll
+  for (int cb = 0; cb < S::kBlocks; ++cb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int ch = 32 * cb + 8 * g + 4 * h;
+      const float o[4] = {w.o[cb][4 * g] * f, w.o[cb][4 * g + 1] * f, w.o[cb][4 * g + 2] * f, w.o[cb][4 * g + 3] * f};
+      if (whole) store_out<T>(a, token, qh, ch, o);
+      else *reinterpret_cast<float4*>(a.part_o + part_row * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
+    }
+  if (h == 0) {
+    if (!whole) a.part_ml[part_row] = make_float2(w.m, w.l);
+    else if (a.lse) a.lse[(int64_t)token * c.hq + qh] = log_sum(w.m, w.l);
+  }
+}
+
+// ---- partial results of a row's key ranges ------------------------------------------------------------------------------
+// A wave joins one row (token, query head).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const int tile_rows, const bool scaled) {
+  const Call& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t job = (int64_t)blockIdx.x * 4 + wave;
+  const int token = (int)(job / c.hq), qh = (int)(job - (int64_t)token * c.hq);
+  if (token >= c.n_tokens) return;
+  const int b = sequence_of_row(c, token);
+  if (b < 0) return;
+  const Seq s = sequence(c, b);
+  const int i_row = token - s.first;
+  if (i_row < 0 || i_row >= s.n) return;
+  const int head = qh / c.group, row = i_row * c.group + qh - head * c.group, t = row / tile_rows, row0 = t * tile_rows;
+  const Range range = tile_range(a, s, row0, min(tile_rows, s.n * c.group - row0));
+  const int n = splits_of(a, range);
+  if (n == 1) return;                                        // written already
+  const int64_t first = ((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits;
+  float m = -kInf;
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, a.part_ml[(first + i) * a.part_rows + row - row0].x);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float ref = m == -kInf ? 0.f : m;
+  float l = 0.f, x0 = 0.f, x1 = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const int64_t at = (first + i) * a.part_rows + row - row0;
+    const float2 ml = a.part_ml[at];
+    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+    l += f * ml.y;
+    if constexpr (D == 128) {
+      const float2 x = reinterpret_cast<const float2*>(a.part_o + at * D)[lane];
+      x0 += f * x.x;
+      x1 += f * x.y;
+    } else {
+      x0 += f * a.part_o[at * D + lane];
+    }
+  }
+  const float f = l == 0.f ? 0.f : (scaled && c.v_scale ? c.v_scale[head] : 1.f) / l;
+  uint8_t* dst = a.out.p + (int64_t)token * a.out.tok + (int64_t)qh * a.out.head;
+  if constexpr (D == 128) reinterpret_cast<uint32_t*>(dst)[lane] = T::pack(x0 * f, x1 * f);
+  else reinterpret_cast<uint16_t*>(dst)[lane] = (uint16_t)T::pack(x0 * f, 0.f);
+  if (a.lse && lane == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(m, l);
+}
+
+template <typename F>
+void by_type(int d, int dtype, bool e4m3, F&& f) {
+  auto by_d = [&](auto t, auto f8) {
+    if (d == 128) f(t, std::integral_constant<int, 128>{}, f8);
+    else f(t, std::integral_constant<int, 64>{}, f8);
+  };
+  auto by_cache = [&](auto t) {
+    if (e4m3) by_d(t, std::true_type{});
+    else by_d(t, std::false_type{});
+  };
+  if (dtype == KV_F16) by_cache(Half{});
+  else by_cache(Brain{});
+}
+
+}  // namespace
+
+void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_rows, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)a.tiles * a.c.hkv * a.splits));
+  by_type(d, dtype, e4m3, [&](auto t, auto dd, auto f8) {
+    if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
+    else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
+  });
+}
+
+void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m3, hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)a.c.n_tokens * a.c.hq + 3) / 4));
+  by_type(d, dtype, false, [&](auto t, auto dd, auto) {
+    merge_kernel<decltype(t), decltype(dd)::value><<<grid, dim3(256), 0, st>>>(a, tile_rows, e4m3);
+  });
+}
+
+}  // namespace paged
+}  // namespace kvx

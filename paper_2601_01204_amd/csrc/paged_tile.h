@@ -1,0 +1,224 @@
+// Pieces of the attention kernels on a paged cache: tiles of keys and values in LDS, and one unit of work, 32 keys x 32 query rows.
+//
+// Products.  S^T = K Q^T and O^T += V^T P^T on the matrix cores (32 x 32 x 16), fp32 accumulators.  The transposed products put a
+// query row in a lane (two lanes, l and l + 32, share one) and its keys in that lane's registers, so that softmax statistics are
+// registers' business with one exchange between the halves, and the probabilities feed the second product without leaving
+// them: register r of half h belongs to key 8 (r / 4) + 4 h + r % 4 of the unit, and V^T is read in that key order.
+//
+// LDS.  Rows of d channels as they lie in the page, in chunks of 16 bytes whose place within the row is exclusive-or'ed with
+// swizzle(row), so that both the row reads of K (a lane a row) and the transposing reads of V (16 lanes four rows of 16 channels
+// each, eight rows for 8-bit values) meet every bank equally often.
+//
+// 8-bit pages are widened as they leave LDS, which is exact; a head's key scale is part of the logit factor, its value scale of the
+// final division.  A row of 8-bit keys is read 16 channels at a time, which serve two matrix instructions: their
+// channels are 32 s + 16 h + 0..7 and 8..15, for the queries too.
+//
+// Softmax.  p = 2^(c s - m) in fp32 with m the largest c s of the row so far, raised only where a key lies more than kGap above it
+// (p stays below 2^kGap, and O and l are rescaled in a rare, wave-uniform branch).  Row sums are taken before
+// the probabilities are rounded for the second product, so that the lse is as exact as the logits.
+#pragma once
+#include "paged_types.h"
+
+#include <type_traits>
+
+namespace kvx {
+namespace paged {
+
+constexpr float kGap = 8.0f;
+constexpr float kInf = __builtin_inff();
+
+template <int ROW_BYTES>
+__device__ __forceinline__ int swizzle(int row) {
+  if constexpr (ROW_BYTES == 256) return ((row & 3) << 2) | ((row >> 2) & 3);
+  else if constexpr (ROW_BYTES == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+  else return (row >> 2) & 3;
+}
+template <int ROW_BYTES>
+__device__ __forceinline__ int lds_offset(int row, int chunk) {
+  return row * ROW_BYTES + ((chunk ^ swizzle<ROW_BYTES>(row)) << 4);
+}
+
+template <int D, bool E4M3>
+struct Shape {
+  static constexpr int kRowBytes = D * (E4M3 ? 1 : 2);
+  static constexpr int kLanesPerRow = kRowBytes / 16;
+  static constexpr int kSteps = D / 16;            // matrix instructions of a unit's first product
+  static constexpr int kBlocks = D / 32;           // 32-channel blocks of the output
+};
+
+// First channel of the octet that half `h` of a wave brings to step s of the first product.
+template <bool E4M3>
+__device__ __forceinline__ int step_channel(int s, int h) {
+  return E4M3 ? 32 * (s >> 1) + 16 * h + 8 * (s & 1) : 16 * s + 8 * h;
+}
+
+// 32 query rows of one wave.
+template <typename T, int D, bool E4M3>
+struct RowBlock {
+  typedef Shape<D, E4M3> S;
+  u32x4 q[S::kSteps];
+  f32x16 o[S::kBlocks];
+  float m, l;                  // in log2 units; l: this lane's half of the keys
+  int lo, hi;                  // keys [lo, hi) are seen by this lane's row
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
+    m = -kInf;
+    l = 0.f;
+  }
+
+  __device__ __forceinline__ void load_queries(const uint8_t* row, int h) {
+#pragma unroll
+    for (int s = 0; s < S::kSteps; ++s) q[s] = *reinterpret_cast<const u32x4*>(row + 2 * step_channel<E4M3>(s, h));
+  }
+
+  // S^T of the unit whose keys' rows begin at `k` in LDS.
+  __device__ __forceinline__ f32x16 logits(const uint8_t* k, int lane) const {
+    const int row = lane & 31, h = lane >> 5;
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    if constexpr (E4M3) {
+#pragma unroll
+      for (int i = 0; i < S::kSteps / 2; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(k + lds_offset<S::kRowBytes>(row, 2 * i + h));
+        s = T::mfma(widen<T>((u32x2){w[0], w[1]}), q[2 * i], s);
+        s = T::mfma(widen<T>((u32x2){w[2], w[3]}), q[2 * i + 1], s);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) s = T::mfma(*reinterpret_cast<const u32x4*>(k + lds_offset<S::kRowBytes>(row, 2 * i + h)), q[i], s);
+    }
+    return s;
+  }
+
+  // V^T fragment: channels 32 b + (lane & 31), keys of step t (16 keys) in the order of the probabilities' registers.
+  static __device__ __forceinline__ u32x4 value_fragment(const uint8_t* v, int lane, int t, int b) {
+    const int h = lane >> 5, j = (lane >> 4) & 1, i = lane & 15;
+    if constexpr (E4M3) {
+      const int row = 16 * t + 4 * h + ((i >> 1) & 3) + 8 * (i >> 3);
+      const uint8_t* p = v + lds_offset<S::kRowBytes>(row, 2 * b + j) + 8 * (i & 1);
+      return widen<T>(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p)));
+    } else {
+      const int row = 16 * t + 4 * h + (i >> 2), chunk = 4 * b + 2 * j + ((i & 3) >> 1);
+      const uint8_t* p0 = v + lds_offset<S::kRowBytes>(row, chunk) + 8 * (i & 1);
+      const uint8_t* p1 = v + lds_offset<S::kRowBytes>(row + 8, chunk) + 8 * (i & 1);
+      const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0));
+      const u32x2 c = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1));
+      return (u32x4){a[0], a[1], c[0], c[1]};
+    }
+  }
+
+  // What the row of this lane does not see becomes -infinity.  key0: first key of the unit; absent: keys without a page.
+  __device__ __forceinline__ void mask(f32x16& s, int key0, uint32_t absent, int h) const {
+    const int first = key0 + 4 * h;
+    absent >>= 4 * h;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int off = 8 * (r >> 2) + (r & 3), key = first + off;
+      s[r] = (key < hi && key >= lo && !((absent >> off) & 1)) ? s[r] : -kInf;
+    }
+  }
+
+  // The unit's probabilities, in place of its logits (c: softmax scale * log2 e); raises m where it has to.
+  __device__ __forceinline__ void soften(f32x16& s, float c) {
+    float top = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
+    {
+      const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = c * fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    }
+    if (__ballot(top > m + kGap)) {                      // (also the first key of a row, whose m is -infinity)
+      const float next = fmaxf(m, top), alpha = next == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - next);
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] *= alpha;
+      l *= alpha;
+      m = next;
+    }
+    const float ref = m == -kInf ? 0.f : m;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref));
+  }
+};
+
+// The page of key `key` of a sequence of `len` tokens (one lane a key): keys behind the end take the last one's.
+__device__ __forceinline__ int32_t page_of_key(const Call& c, int b, int key, int len) {
+  return page_of(c, b, min(key, len - 1) >> c.page_shift);
+}
+__device__ __forceinline__ int64_t row_offset(const Call& c, int32_t page, int key) {
+  return (page < 0 ? 0 : page) * c.page_stride + (int64_t)(key & ((1 << c.page_shift) - 1)) * c.slot_stride;
+}
+
+// Which rows a workgroup works on: row tile `t` of sequence `b`; false: none.
+__device__ __forceinline__ bool find_tile(const AttendArgs& a, int tile, int tile_rows, int& b, int& t) {
+  if (a.tiles_per_seq > 0) {
+    b = tile / a.tiles_per_seq;
+    t = tile - b * a.tiles_per_seq;
+    return true;
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;                                        // tiles of the sequences passed
+  for (int base = 0; base < a.c.n_seqs; base += 64) {
+    const int s = base + lane;
+    int mine = 0;
+    if (s < a.c.n_seqs) mine = (sequence(a.c, s).n * a.c.group + tile_rows - 1) / tile_rows;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const int total = __shfl(upto, 63);
+    if (tile < before + total) {
+      const uint64_t behind = __ballot(before + upto <= tile);
+      const int at = __popcll(behind);                   // ascending, so these are the lanes in front
+      b = base + at;
+      t = tile - before - (at ? __shfl(upto, at - 1) : 0);
+      return true;
+    }
+    before += total;
+  }
+  return false;
+}
+// The tile number of row tile t of sequence b (what find_tile inverts).
+__device__ __forceinline__ int tile_number(const AttendArgs& a, int b, int t, int tile_rows) {
+  if (a.tiles_per_seq > 0) return b * a.tiles_per_seq + t;
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int base = 0; base < b; base += 64) {
+    const int s = base + lane;
+    int mine = s < b ? (sequence(a.c, s).n * a.c.group + tile_rows - 1) / tile_rows : 0;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) mine += __shfl_xor(mine, o);
+    before += mine;
+  }
+  return before + t;
+}
+
+// The keys that row tile t of a sequence reads: [lo, hi), lo on a multiple of 64.
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range tile_range(const AttendArgs& a, const Seq& s, int row0, int n_rows) {
+  const int place0 = s.len - s.n + row0 / a.c.group, place1 = s.len - s.n + (row0 + n_rows - 1) / a.c.group;
+  Range r;
+  r.hi = a.causal ? min(s.len, place1 + 1) : s.len;
+  r.lo = a.window > 0 ? max(0, place0 + 1 - a.window) & ~63 : 0;
+  return r;
+}
+// How many key ranges that is; the last range of the launch ends where the tile's keys do.
+__device__ __forceinline__ int splits_of(const AttendArgs& a, const Range& r) {
+  return r.hi > r.lo ? min(a.splits, (r.hi - r.lo + a.split_keys - 1) / a.split_keys) : 1;
+}
+__device__ __forceinline__ int split_end(const AttendArgs& a, const Range& r, int split) {
+  return split == a.splits - 1 ? r.hi : min(r.hi, r.lo + (split + 1) * a.split_keys);
+}
+
+}  // namespace paged
+}  // namespace kvx

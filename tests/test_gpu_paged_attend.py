@@ -1,0 +1,191 @@
+"""Attention over a paged cache against its 64-bit definition: kinds of rows, heads, types, layouts, lengths and masks."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as po
+from tests import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+
+def run(case, causal=True, window=0, weights=False, scale=0.0, q=None, max_new=None):
+    """Makes the call, checks out, lse and weights against the definition; returns the handle's status."""
+    h, pages, batch = case.handle(softmax_scale=scale), None, case.batch(max_new=max_new)
+    case.weights.copy_(torch.rand(case.weights.shape, generator=torch.Generator().manual_seed(5)))
+    before = case.weights.cpu().double().numpy()
+    pages = case.pages()
+    q = case.rows(case.hq) if q is None else q
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((case.n_tokens, case.hq), 7.0, device=case.device)
+    w_out = torch.full_like(case.weights, 7.0)
+    h.attend(pages, batch, q, out, lse=lse, causal=causal, window=window, weights_out=w_out if weights else None)
+    torch.cuda.synchronize()
+    scale = scale or 1 / math.sqrt(case.d)
+    ref, rl, gained, absolute, reach = po.attend(case.pool, q.float().cpu().numpy(), case.start, case.lens, scale, causal, window,
+                                                 None if case.k_scale is None else case.k_scale.numpy(), None if case.v_scale is None else case.v_scale.numpy())
+    few = max([0] + case.new) * case.hq // case.hkv <= 32
+    b_out, b_lse, b_w = pu.attend_bounds(case, ref, absolute, rl, gained, reach, few)
+    n = case.start[-1]
+    pu.check(out.float().cpu().numpy()[:n], ref[:n], b_out[:n], "out")
+    pu.check(lse.cpu().numpy()[:n], rl[:n], b_lse[:n], "lse")
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all(), "rows of no sequence are left alone"
+    if weights:
+        live = np.zeros(before.shape, bool)
+        for b, t in enumerate(case.lens):
+            for j in range(t):
+                p = po.place(case.pool, b, j)
+                if p is not None:
+                    live[p[0], :, p[1]] = True
+        got = w_out.cpu().double().numpy()
+        assert (got[~live] == 7).all(), "weights of other slots are left alone"
+        pu.check(got[live], (before + gained)[live], np.broadcast_to(b_w, before.shape)[live], "weights")
+    status = h.status()
+    h.close()
+    return status
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_types_and_layouts_single_tokens(dtype, cache, d, heads_first):
+    assert run(pu.Case([1, 33, 517, 64, 200], [1] * 5, hq=8, hkv=2, d=d, dtype=dtype, cache=cache, heads_first=heads_first, seed=d), weights=True) == 0
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_types_and_layouts_chunks(dtype, cache, d, heads_first):
+    assert run(pu.Case([300, 97], [150, 97], hq=4, hkv=2, d=d, page=32, dtype=dtype, cache=cache, heads_first=heads_first, seed=d + 1), weights=True) == 0
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (5, 5), (6, 1), (9, 3), (16, 1), (24, 2), (40, 1), (128, 1)])
+@pytest.mark.parametrize("new", [1, 3, 45])
+def test_head_groups(hq, hkv, new):
+    assert run(pu.Case([130, 45 + new], [new, new], hq=hq, hkv=hkv, page=8, seed=hq + new), weights=True) == 0
+
+
+@pytest.mark.parametrize("lens,new", [
+    ([1], [1]), ([2], [2]), ([31], [1]), ([32], [1]), ([33], [1]), ([63], [2]), ([64], [8]), ([65], [16]), ([127], [1]), ([129], [31]),
+    ([128], [128]), ([129], [129]), ([257], [255]), ([700], [33]), ([64, 1, 0, 65], [1, 1, 0, 1]), ([64, 1, 0, 65, 200], [40, 1, 0, 0, 129]),
+    ([0], [0]), ([5, 0, 0], [0, 0, 0])])
+@pytest.mark.parametrize("page", [8, 64, 1024])
+def test_lengths(lens, new, page):
+    assert run(pu.Case(lens, new, page=page, seed=sum(lens)), weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [1, 7, 50, 140])
+@pytest.mark.parametrize("window", [1, 5, 64, 100, 10000])
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows(new, window, causal):
+    assert run(pu.Case([400, new, 173], [new, new, 3], hq=2, hkv=1, page=16, seed=window), causal=causal, window=window, weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [3, 140])
+def test_not_causal(new):
+    assert run(pu.Case([400, new, 173], [new, new, 3], hq=2, hkv=2, page=16, seed=new), causal=False, weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [4, 60])
+def test_rows_that_see_nothing(new):
+    """More new tokens than cached ones: the first rows' places lie before the sequence, they are zero and their lse -infinity."""
+    case = pu.Case([new - 3, 20], [new, 1], hq=4, hkv=2, page=8, seed=new)
+    run(case, weights=True)
+
+
+@pytest.mark.parametrize("B,new", [(70, 1), (130, 1), (67, 2)])
+def test_more_sequences_than_lanes(B, new):
+    rng = np.random.default_rng(B)
+    assert run(pu.Case(list(rng.integers(new, 90, B)), [new] * B, hq=2, hkv=1, page=8, seed=B), weights=True) == 0
+
+
+def test_uneven_chunks_are_counted_out():
+    """One long and many short ones: fewer row tiles than sequences times the longest one's."""
+    new = [300] + [0, 1, 2, 5, 130] * 14
+    lens = [n + (i * 37) % 150 for i, n in enumerate(new)]
+    assert run(pu.Case(lens, new, hq=2, hkv=1, page=16, seed=1), weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [1, 80])
+def test_long_caches_in_ranges(new):
+    """Keys enough for several ranges, whose partial results are joined."""
+    assert run(pu.Case([9000, 2500, 70], [new, 1, new], hq=4, hkv=2, d=128, page=64, seed=new), weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_pages_outside_the_pool_hold_nothing(new):
+    case = pu.Case([300, 300, 90], [new, new, 1], hq=4, hkv=2, page=16, seed=3)
+    for b, e, bad in ((0, 3, -1), (0, 4, case.n_pages), (1, 0, 1 << 30), (1, 11, -(1 << 31)), (2, 5, -7)):
+        case.pool["table"][b, e] = bad
+    case.table.copy_(torch.from_numpy(case.pool["table"]))
+    assert run(case, weights=True) == 1
+    for e in range(6):                                   # a sequence with no page at all
+        case.pool["table"][2, e] = -1
+    case.table.copy_(torch.from_numpy(case.pool["table"]))
+    assert run(case, weights=True) == 1
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_rows_behind_the_last_sequence(new):
+    assert run(pu.Case([100, 90], [new, new], extra_rows=9, seed=2)) == 0
+
+
+@pytest.mark.parametrize("new", [1, 33])
+def test_large_logits(new):
+    """Logits of hundreds: one key takes nearly everything, and the largest comes late."""
+    case = pu.Case([500], [new], hq=2, hkv=1, d=64, dtype="f16", seed=6)
+    assert run(case, q=case.rows(2, scale=40.0), weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_scale_of_the_configuration(new):
+    assert run(pu.Case([150], [new], seed=8), scale=0.37, weights=True) == 0
+
+
+def test_strides_of_rows_and_pages():
+    """Queries as parts of wider rows, pages as parts of wider pages, a page table as part of a wider one."""
+    case = pu.Case([150, 70], [40, 3], hq=4, hkv=2, d=64, seed=9)
+    wide = torch.randn(case.n_tokens, 9, 96, device=case.device).to(torch.bfloat16)
+    q = wide[:, 2:6, 16:80]
+    room_k, room_v = (torch.full((case.n_pages, case.page, 3, 96), float("nan"), device=case.device, dtype=torch.bfloat16) for _ in range(2))
+    room_k[:, :, 1:, 32:] = case.k
+    room_v[:, :, 1:, 32:] = case.v
+    case.k, case.v = room_k[:, :, 1:, 32:], room_v[:, :, 1:, 32:]
+    table = torch.full((2, case.table.shape[1] + 5), 1 << 29, dtype=torch.int32, device=case.device)
+    table[:, :case.table.shape[1]] = case.table
+    case.table = table
+    assert run(case, q=q, weights=True) == 0
+
+
+def test_a_prefix_shared_by_sequences():
+    case = pu.Case([200, 180, 64], [2, 1, 1], page=32, seed=10)
+    case.pool["table"][1, :3] = case.pool["table"][0, :3]
+    case.pool["table"][2, :2] = case.pool["table"][0, :2]
+    case.table.copy_(torch.from_numpy(case.pool["table"]))
+    assert run(case) == 0
+
+
+def test_weights_in_place():
+    case = pu.Case([200, 90], [1, 20], hq=4, hkv=2, page=16, seed=11)
+    h, q = case.handle(), case.rows(4)
+    out = torch.empty_like(q)
+    apart = torch.zeros_like(case.weights)
+    h.attend(case.pages(), case.batch(), q, out, weights_out=apart)
+    pages = case.pages()
+    h.attend(pages, case.batch(), q, out, weights_out=pages.weights)
+    torch.cuda.synchronize()
+    assert torch.equal(apart, case.weights) and float(apart.sum()) > 1
+    assert abs(float(apart.double().sum()) - 4 * 21) < 1e-3          # every row gives out a weight of 1
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_the_same_call_twice_gives_the_same_bits(new):
+    case = pu.Case([3000, 170], [new, new], hq=8, hkv=2, d=128, seed=12)
+    h, q = case.handle(), case.rows(8)
+    outs, ws = [torch.empty_like(q) for _ in range(3)], [torch.zeros_like(case.weights) for _ in range(3)]
+    for o, w in zip(outs, ws):
+        h.attend(case.pages(), case.batch(), q, o, weights_out=w)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and torch.equal(ws[0], ws[1]) and torch.equal(ws[0], ws[2])
