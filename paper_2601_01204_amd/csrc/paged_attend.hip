@@ -323,12 +323,16 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
 }
 
 // ---- partial results of a row's key ranges ------------------------------------------------------------------------------
-// A wave joins one row (token, query head).
-template <typename T, int D>
+// WAVES waves join one row (token, query head): a lane has four channels, 256 / D lane groups of a wave take a range each and the
+// next ranges after it, four loads ahead.  One wave is enough for a few ranges; 128 of them took one wave 58 us (128 rows, d = 128,
+// two channels a lane, one range after the other).
+template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const int tile_rows, const bool scaled) {
+  constexpr int kLanes = D / 4, kGroups = 64 / kLanes * WAVES;      // lanes of a range, ranges at a time
+  __shared__ float join[WAVES > 1 ? WAVES : 1][D + 1];
   const Call& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t job = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t job = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   const int token = (int)(job / c.hq), qh = (int)(job - (int64_t)token * c.hq);
   if (token >= c.n_tokens) return;
   const int b = sequence_of_row(c, token);
@@ -340,30 +344,56 @@ __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const in
   const Range range = tile_range(a, s, row0, min(tile_rows, s.n * c.group - row0));
   const int n = splits_of(a, range);
   if (n == 1) return;                                        // written already
-  const int64_t first = ((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits;
+  const int64_t first = (((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits) * a.part_rows + row - row0;
+  const float2* const ml = a.part_ml + first;
+  const float* const part = a.part_o + first * D;
   float m = -kInf;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, a.part_ml[(first + i) * a.part_rows + row - row0].x);
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, ml[(int64_t)i * a.part_rows].x);
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   const float ref = m == -kInf ? 0.f : m;
-  float l = 0.f, x0 = 0.f, x1 = 0.f;
-  for (int i = 0; i < n; ++i) {
-    const int64_t at = (first + i) * a.part_rows + row - row0;
-    const float2 ml = a.part_ml[at];
-    const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-    l += f * ml.y;
-    if constexpr (D == 128) {
-      const float2 x = reinterpret_cast<const float2*>(a.part_o + at * D)[lane];
-      x0 += f * x.x;
-      x1 += f * x.y;
-    } else {
-      x0 += f * a.part_o[at * D + lane];
+  const int ch = lane % kLanes * 4, group = (WAVES == 1 ? 0 : wave * (64 / kLanes)) + lane / kLanes;
+  float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = group; i < n; i += kGroups) {
+    const float2 w = ml[(int64_t)i * a.part_rows];
+    const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)i * a.part_rows * D + ch);
+    const float f = __builtin_amdgcn_exp2f(w.x - ref);
+    l += f * w.y;
+    x[0] += f * y.x;
+    x[1] += f * y.y;
+    x[2] += f * y.z;
+    x[3] += f * y.w;
+  }
+#pragma unroll
+  for (int o = kLanes; o < 64; o <<= 1) {
+    l += __shfl_xor(l, o);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], o);
+  }
+  if constexpr (WAVES > 1) {
+    if (lane < kLanes) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) join[wave][ch + e] = x[e];
+      if (lane == 0) join[wave][D] = l;
+    }
+    __syncthreads();                                         // (a workgroup's waves have the same row: none has left)
+    if (wave > 0) return;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      l += join[i][D];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += join[i][ch + e];
     }
   }
+  if (lane >= kLanes) return;
   const float f = l == 0.f ? 0.f : (scaled && c.v_scale ? c.v_scale[head] : 1.f) / l;
-  uint8_t* dst = a.out.p + (int64_t)token * a.out.tok + (int64_t)qh * a.out.head;
-  if constexpr (D == 128) reinterpret_cast<uint32_t*>(dst)[lane] = T::pack(x0 * f, x1 * f);
-  else reinterpret_cast<uint16_t*>(dst)[lane] = (uint16_t)T::pack(x0 * f, 0.f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= f;
+  store_out<T>(a, token, qh, ch, x);
   if (a.lse && lane == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(m, l);
 }
 
@@ -392,9 +422,10 @@ void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_ro
 }
 
 void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m3, hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)a.c.n_tokens * a.c.hq + 3) / 4));
+  const int64_t rows = (int64_t)a.c.n_tokens * a.c.hq;
   by_type(d, dtype, false, [&](auto t, auto dd, auto) {
-    merge_kernel<decltype(t), decltype(dd)::value><<<grid, dim3(256), 0, st>>>(a, tile_rows, e4m3);
+    if (a.splits > 8) merge_kernel<decltype(t), decltype(dd)::value, 4><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a, tile_rows, e4m3);
+    else merge_kernel<decltype(t), decltype(dd)::value, 1><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st>>>(a, tile_rows, e4m3);
   });
 }
 
