@@ -61,7 +61,8 @@ def _is(t, dtype):
 
 
 def _int_array(t, name, n=None):
-    assert _is(t, "int32") and t.dim() == 1 and t.is_contiguous() and (n is None or t.numel() == n), f"{name} must be a contiguous int32 vector" + (f" of {n}" if n else "")
+    if not _is(t, "int32") or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise AssertionError(f"{name} must be a contiguous int32 vector" + ("" if n is None else f" of {n}"))
     return t.data_ptr()
 
 
@@ -135,6 +136,10 @@ class KvPaged:
             raise KvError(rc, self.lib.kv_paged_last_error(None).decode())
         c.rope_freqs = None
         self._hq, self._hkv, self._d = c.n_q_heads, c.n_kv_heads, c.head_dim
+        self._append, self._attend, self._evict = self.lib.kv_paged_append, self.lib.kv_paged_attend, self.lib.kv_paged_evict
+        self._records = [KvRows() for _ in range(4)]      # of the running call
+        self._refs = [C.byref(r) for r in self._records]
+        self._type = None                                 # the tensors' dtype, once one has been seen
         names = {KV_BF16: "torch.bfloat16", KV_F16: "torch.float16", KV_E4M3: "torch.float8_e4m3fn"}
         self._dtype, self._form = names[c.dtype], (c.n_kv_heads, c.head_dim, c.page_size, names[c.cache_dtype])
 
@@ -143,42 +148,54 @@ class KvPaged:
             raise KvError(rc, self.lib.kv_paged_last_error(self._h).decode())
 
     def _pages(self, pages, batch):
-        assert pages.form == self._form, f"the pool's (heads, channels, page size, type) are {pages.form}, the handle's {self._form}"
-        assert batch.device == pages.device and batch.n_seqs <= pages.n_seqs, "the batch's device or sequences are not the page table's"
+        if pages.form != self._form:
+            raise AssertionError(f"the pool's (heads, channels, page size, type) are {pages.form}, the handle's {self._form}")
+        if batch.device != pages.device or batch.n_seqs > pages.n_seqs:
+            raise AssertionError("the batch's device or sequences are not the page table's")
 
-    def _rows(self, t, heads, batch, name):
-        shape, stride = t.shape, t.stride()
-        if batch.n_tokens == 0 and tuple(shape) == (0, heads, self._d):
+    def _rows(self, t, heads, batch, name, place):
+        """Address and strides of a call's tensor in the handle's record number `place` (a call takes microseconds, and so does making a record)."""
+        n, d = batch.n_tokens, self._d
+        if t.shape != (n, heads, d) or t.dtype is not self._type or t.device != batch.device:
+            if t.shape != (n, heads, d) or str(t.dtype) != self._dtype or t.device != batch.device:
+                raise AssertionError(f"{name} must be [{n}, {heads}, {d}] {self._dtype} on {batch.device}")
+            self._type = t.dtype
+        if n == 0:
             return None                                   # (an empty tensor has no address)
-        assert len(shape) == 3 and shape[0] == batch.n_tokens and shape[1] == heads and shape[2] == self._d and stride[2] == 1, \
-            f"{name} must be [{batch.n_tokens}, {heads}, {self._d}] with contiguous channels"
-        assert str(t.dtype) == self._dtype and t.device == batch.device, f"{name} must be {self._dtype} on {batch.device}"
-        ts = stride[0] if shape[0] > 1 else max(stride[0], self._d)
-        hs = stride[1] if shape[1] > 1 else max(stride[1], self._d)
-        return C.byref(KvRows(t.data_ptr(), ts, hs))
+        ts, hs, one = t.stride()
+        if one != 1:
+            raise AssertionError(f"{name} must have contiguous channels")
+        r = self._records[place]
+        r.data = t.data_ptr()
+        r.tok_stride = ts if n > 1 or ts > d else d       # (a dimension of one element may carry any stride)
+        r.head_stride = hs if heads > 1 or hs > d else d
+        return self._refs[place]
 
     def append(self, pages, batch, k, v, q=None, q_out=None, positions=None, hip_stream: int = 0):
         """kv_paged_append.  k, v: [tokens, key heads, d]; q, q_out: [tokens, query heads, d] (q_out may be q); positions: int32 [tokens]."""
         self._pages(pages, batch)
-        rq = self._rows(q, self._hq, batch, "q") if q is not None else None
-        ro = self._rows(q_out, self._hq, batch, "q_out") if q_out is not None else None
+        rq = self._rows(q, self._hq, batch, "q", 0) if q is not None else None
+        ro = self._rows(q_out, self._hq, batch, "q_out", 1) if q_out is not None else None
         p = None
         if positions is not None:
             assert positions.device == batch.device
             p = _int_array(positions, "positions", batch.n_tokens)
-        self._check(self.lib.kv_paged_append(self._h, pages.ref, batch.ref, p, rq, ro, self._rows(k, self._hkv, batch, "k"),
-                                             self._rows(v, self._hkv, batch, "v"), hip_stream))
+        rc = self._append(self._h, pages.ref, batch.ref, p, rq, ro, self._rows(k, self._hkv, batch, "k", 2), self._rows(v, self._hkv, batch, "v", 3), hip_stream)
+        if rc:
+            self._check(rc)
 
     def attend(self, pages, batch, q, out, lse=None, causal=True, window: int = 0, weights_out=None, hip_stream: int = 0):
         """kv_paged_attend.  q, out: [tokens, query heads, d]; lse: fp32 [tokens, query heads]; weights_out: as pages.weights."""
         self._pages(pages, batch)
         p_lse = None
         if lse is not None:
-            assert _is(lse, "float32") and tuple(lse.shape) == (batch.n_tokens, self._hq) and lse.is_contiguous() and lse.device == batch.device, \
+            assert _is(lse, "float32") and lse.shape == (batch.n_tokens, self._hq) and lse.is_contiguous() and lse.device == batch.device, \
                 "lse must be a contiguous float32 [tokens, query heads]"
             p_lse = lse.data_ptr()
-        self._check(self.lib.kv_paged_attend(self._h, pages.ref, batch.ref, self._rows(q, self._hq, batch, "q"), self._rows(out, self._hq, batch, "out"),
-                                             p_lse, 1 if causal else 0, window, self._meta(pages, weights_out, pages.weights, "weights"), hip_stream))
+        rc = self._attend(self._h, pages.ref, batch.ref, self._rows(q, self._hq, batch, "q", 0), self._rows(out, self._hq, batch, "out", 1), p_lse,
+                          1 if causal else 0, window, None if weights_out is None else self._meta(pages, weights_out, pages.weights, "weights"), hip_stream)
+        if rc:
+            self._check(rc)
 
     @staticmethod
     def _meta(pages, t, like, name):
@@ -195,7 +212,7 @@ class KvPaged:
         if lens_out is not None:
             assert lens_out.device == batch.device
             p_lens = _int_array(lens_out, "lens_out", batch.n_seqs)
-        self._check(self.lib.kv_paged_evict(self._h, pages.ref, batch.ref, budget, sinks, recent, self._meta(pages, weights_out, pages.weights, "weights"),
+        self._check(self._evict(self._h, pages.ref, batch.ref, budget, sinks, recent, self._meta(pages, weights_out, pages.weights, "weights"),
                                             self._meta(pages, ids_out, pages.ids, "ids"), p_lens, hip_stream))
 
     def status(self) -> int:
