@@ -420,8 +420,9 @@ typedef struct kv_pages {
   int64_t table_stride;
   const float* k_scale;     /* device, [Hkv], KV_E4M3: a stored key times its head's scale is the  */
   const float* v_scale;     /* key (values likewise); NULL: 1.  Positive and finite                */
-  float* weights;           /* device, [n_pages][Hkv][page_size]: weight each cached token has received; NULL: not kept */
-  int32_t* ids;             /* device, [n_pages][Hkv][page_size]: which token of its sequence a slot holds; NULL: not kept */
+  float* weights;           /* device, [n_pages][Hkv][page_size]: weight each cached token has received; NULL: not kept. */
+  int32_t* ids;             /* device, [n_pages][Hkv][page_size]: which token of its sequence a slot holds; NULL: not kept. */
+                            /* Both, and what calls write in their layout, 16-byte aligned            */
 } kv_pages;
 
 /* The sequences of a call and their new tokens: rows q_start[s] .. q_start[s + 1] - 1 of the call's tensors are the

@@ -160,9 +160,9 @@ int check_call(kv_paged* h, const char* call, const kv_pages* p, const kv_paged_
     return fail(h, KV_E_INVAL, "%s: pages_per_seq must be >= 1 and table_stride no smaller", call);
   if (((int64_t)p->pages_per_seq << h->page_shift) < b->max_len)
     return fail(h, KV_E_RANGE, "%s: %d pages of %d slots hold fewer than max_len = %d tokens", call, p->pages_per_seq, c.page_size, b->max_len);
-  if (((uintptr_t)p->page_table | (uintptr_t)b->q_start | (uintptr_t)b->kv_lens | (uintptr_t)b->seen | (uintptr_t)p->weights | (uintptr_t)p->ids |
-       (uintptr_t)p->k_scale | (uintptr_t)p->v_scale) & 3)
+  if (((uintptr_t)p->page_table | (uintptr_t)b->q_start | (uintptr_t)b->kv_lens | (uintptr_t)b->seen | (uintptr_t)p->k_scale | (uintptr_t)p->v_scale) & 3)
     return fail(h, KV_E_INVAL, "%s: arrays must be 4-byte aligned", call);
+  if (((uintptr_t)p->weights | (uintptr_t)p->ids) & 15) return fail(h, KV_E_INVAL, "%s: weights and ids must be 16-byte aligned", call);
   Call& o = *out;
   o.k = (uint8_t*)p->k;
   o.v = (uint8_t*)p->v;
@@ -264,7 +264,6 @@ int kv_paged_init(const kv_paged_config* cfg, kv_paged** out) {
   hipError_t e = hipGetDevice(&h->device);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, h->device);
   if (e == hipSuccess && cus < 1) e = hipErrorInvalidDevice;
-  if (e == hipSuccess) e = prepare_evict();
   if (e != hipSuccess) {
     rc = fail(nullptr, KV_E_HIP, "kv_paged_init: no HIP device: %s", hipGetErrorString(e));
     (void)hipGetLastError();
@@ -350,7 +349,8 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   if ((rc = check_rows(h, "kv_paged_attend", "q", batch, q, &a.q)) != KV_OK || (rc = check_rows(h, "kv_paged_attend", "out", batch, out, &a.out)) != KV_OK) return rc;
   if (window < 0) return fail(h, KV_E_INVAL, "kv_paged_attend: window must be >= 0");
   if (weights_out && !a.c.weights) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out needs pages->weights");
-  if (((uintptr_t)lse | (uintptr_t)weights_out) & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse and weights_out must be 4-byte aligned");
+  if ((uintptr_t)lse & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse must be 4-byte aligned");
+  if ((uintptr_t)weights_out & 15) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out must be 16-byte aligned");
   hipStream_t st = (hipStream_t)hip_stream;
   const kv_paged_config& c = h->cfg;
   const bool e4m3 = c.cache_dtype == KV_E4M3;
@@ -383,7 +383,8 @@ int kv_paged_evict(kv_paged* h, const kv_pages* pages, const kv_paged_batch* bat
   if (rc != KV_OK) return rc;
   if (!a.c.weights || !a.c.ids) return fail(h, KV_E_INVAL, "kv_paged_evict: needs pages->weights and pages->ids");
   if (!weights_out || !ids_out || !lens_out) return fail(h, KV_E_INVAL, "kv_paged_evict: weights_out, ids_out or lens_out is NULL");
-  if (((uintptr_t)weights_out | (uintptr_t)ids_out | (uintptr_t)lens_out) & 3) return fail(h, KV_E_INVAL, "kv_paged_evict: arrays must be 4-byte aligned");
+  if ((uintptr_t)lens_out & 3) return fail(h, KV_E_INVAL, "kv_paged_evict: lens_out must be 4-byte aligned");
+  if (((uintptr_t)weights_out | (uintptr_t)ids_out) & 15) return fail(h, KV_E_INVAL, "kv_paged_evict: weights_out and ids_out must be 16-byte aligned");
   if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
     return fail(h, KV_E_INVAL, "kv_paged_evict: budget must be >= 1, sinks and recent >= 0 and together no more than budget");
   a.max_moves = std::max(1, std::min(budget, a.c.max_len - budget));

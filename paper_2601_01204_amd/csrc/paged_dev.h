@@ -77,7 +77,6 @@ void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m
 void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st);
 // arrived: [n_seqs], zero before and after
 void launch_evict(const EvictArgs& a, int d, bool e4m3, int32_t* arrived, hipStream_t st);
-hipError_t prepare_evict();      // once per device
 
 }  // namespace paged
 }  // namespace kvx

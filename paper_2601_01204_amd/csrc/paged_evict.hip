@@ -20,20 +20,11 @@ namespace paged {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kLdsKeys = 32768;                 // longer caches read their keys again in every pass
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
 constexpr int kFewMoves = 256;
 
-// Index of slot j in weights and ids; -1: no page.
-__device__ __forceinline__ int64_t meta_index(const Call& c, int b, int head, int j) {
-  const int32_t page = page_of(c, b, j >> c.page_shift);
-  return page < 0 ? -1 : (((int64_t)page * c.hkv + head) << c.page_shift) + (j & ((1 << c.page_shift) - 1));
-}
-__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, int64_t at, int seen) {
-  if (at < 0) return 0u;
-  const int32_t id = a.c.ids[at];
+__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, int32_t id, float w, int seen) {
   if (id < a.sinks || id >= seen - a.recent) return kProtected;
-  const float w = a.c.weights[at];
   if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);            // the two zeros are one weight
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);                 // -infinity: 0x007FFFFF, +infinity: 0xFF800000
@@ -62,60 +53,185 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int head, c
   }
 }
 
-// Sum over the waves of a workgroup in front of this one, and the total; every wave brings `mine`.
-__device__ __forceinline__ int before_me(int mine, int wave, int* sums, int& total) {
+// Sums over the waves of a workgroup in front of this one, of two counts that every wave brings; totals too.
+struct Counts {
+  int x, y;
+};
+__device__ __forceinline__ Counts before_me(Counts mine, int wave, int2* sums, Counts* total = nullptr) {
   __syncthreads();                              // the last use of sums is over
-  if ((threadIdx.x & 63) == 0) sums[wave] = mine;
+  if ((threadIdx.x & 63) == 0) sums[wave] = make_int2(mine.x, mine.y);
   __syncthreads();
-  int before = 0;
-  total = 0;
+  int2 all[kWaves];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) all[i] = sums[i];
+  Counts before{0, 0}, sum{0, 0};
+#pragma unroll
   for (int i = 0; i < kWaves; ++i) {
-    const int x = sums[i];
-    before += i < wave ? x : 0;
-    total += x;
+    before.x += i < wave ? all[i].x : 0;
+    before.y += i < wave ? all[i].y : 0;
+    sum.x += all[i].x;
+    sum.y += all[i].y;
   }
+  if (total) *total = sum;
   return before;
 }
 
-template <int ROW_BYTES>
-__global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, const int lds_keys, const bool move_here, int32_t* const arrived) {
-  extern __shared__ uint32_t keys[];            // [lds_keys]
-  __shared__ int hist[2048];
-  __shared__ int sums[kWaves];
-  __shared__ int found[2];
+// A thread has groups of four neighbouring slots (pages begin on a multiple of eight).  NIT > 0: the keys of its NIT groups stay in its
+// registers, up to kHold groups with the weights and ids they come from; NIT = 0: caches of any length, whose keys are formed again in
+// every pass.
+constexpr int kHold = 4;
+
+template <int ROW_BYTES, int NIT>
+__global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, const bool move_here, int32_t* const arrived) {
+  constexpr bool kKeep = NIT > 0 && NIT <= kHold;
+  constexpr int kRegs = NIT > 0 ? NIT : 1;
+  __shared__ __align__(16) int hist[2048];
+  __shared__ __align__(16) int2 sums[kWaves];
+  __shared__ int found[3];
   const Call& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = blockIdx.x % c.hkv, b = blockIdx.x / c.hkv;
   const Seq s = sequence(c, b);
-  const int len = s.len, budget = a.budget, seen = c.seen[b];
-  const bool over = len > budget;
-  // the new length is written by the sequence's last workgroup to get here: lens_out may be the lengths that all of them read
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    __threadfence();
-    if (atomicAdd(&arrived[b], 1) == c.hkv - 1) {
-      arrived[b] = 0;
-      a.lens_out[b] = over ? budget : len;
+  const int len = s.len, budget = a.budget, seen = c.seen[b], mask = (1 << c.page_shift) - 1;
+  const bool over = len > budget, in_place = a.weights_out == c.weights && a.ids_out == c.ids;
+  int2* const moves = a.moves + (int64_t)blockIdx.x * a.max_moves;
+  // a wave has a contiguous part of the slots, 256 at a time
+  const int its = (len + 4 * kThreads - 1) / (4 * kThreads), part = its * 256, j0 = min(len, wave * part), j1 = min(len, j0 + part);
+
+  struct Group {
+    int32_t page;
+    int32_t id[4];
+    float w[4];
+  };
+  auto slot_of = [&](int it) { return j0 + 256 * it + 4 * lane; };
+  auto index_of = [&](int32_t page, int j) { return (((int64_t)page * c.hkv + head) << c.page_shift) + (j & mask); };
+  auto load_page = [&](Group& g, int it) { g.page = slot_of(it) < j1 ? page_of(c, b, slot_of(it) >> c.page_shift) : -1; };
+  auto load_rest = [&](Group& g, int it) {
+    int4 i4 = make_int4(0, 0, 0, 0);
+    float4 w4 = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g.page >= 0) {
+      const int64_t at = index_of(g.page, slot_of(it));
+      i4 = *reinterpret_cast<const int4*>(c.ids + at);
+      w4 = *reinterpret_cast<const float4*>(c.weights + at);
+    }
+    g.id[0] = i4.x; g.id[1] = i4.y; g.id[2] = i4.z; g.id[3] = i4.w;
+    g.w[0] = w4.x; g.w[1] = w4.y; g.w[2] = w4.z; g.w[3] = w4.w;
+  };
+  auto form_keys = [&](const Group& g, int it, uint32_t (&k)[4]) {
+    if (slot_of(it) < j1 && g.page < 0) note_bad_page(c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = g.page >= 0 ? key_of(a, g.id[e], g.w[e], seen) : 0u;
+  };
+  // the slots of `wanted` (a bit each of a group's four) go to weights_out and ids_out
+  auto store = [&](const Group& g, int it, uint32_t wanted) {
+    if (g.page < 0 || !wanted) return;
+    const int64_t at = index_of(g.page, slot_of(it));
+    if (wanted == 15u) {
+      *reinterpret_cast<int4*>(a.ids_out + at) = make_int4(g.id[0], g.id[1], g.id[2], g.id[3]);
+      *reinterpret_cast<float4*>(a.weights_out + at) = make_float4(g.w[0], g.w[1], g.w[2], g.w[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((wanted >> e) & 1) {
+          a.ids_out[at + e] = g.id[e];
+          a.weights_out[at + e] = g.w[e];
+        }
+    }
+  };
+
+  uint32_t key[kRegs][4];
+  Group held[kKeep ? kRegs : 1];
+  if constexpr (kKeep) {
+    // every load of a kind is on its way before the first is used
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) load_page(held[i], i);
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) load_rest(held[i], i);
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) form_keys(held[i], i, key[i]);
+  } else if constexpr (NIT > 0) {
+#pragma unroll
+    for (int base = 0; base < NIT; base += 4) {
+      Group g[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_page(g[i], base + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_rest(g[i], base + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) form_keys(g[i], base + i, key[base + i]);
     }
   }
-  int2* const moves = a.moves + (int64_t)blockIdx.x * a.max_moves;
-  if (!over) {
-    for (int j = threadIdx.x; j < len; j += kThreads) {
-      const int64_t at = meta_index(c, b, head, j);
-      if (at < 0) {
-        note_bad_page(c);
-      } else {
-        a.weights_out[at] = c.weights[at];
-        a.ids_out[at] = c.ids[at];
+  // f(group number, first slot, keys); all lanes of a wave together, slots from j1 on are nobody's
+  auto each = [&](auto&& f) {
+    if constexpr (NIT > 0) {
+#pragma unroll
+      for (int i = 0; i < NIT; ++i)
+        if (i < its) f(i, slot_of(i), key[i]);
+    } else {
+      for (int i = 0; i < its; ++i) {
+        Group g;
+        load_page(g, i);
+        load_rest(g, i);
+        uint32_t k[4];
+        form_keys(g, i, k);
+        f(i, slot_of(i), k);
       }
     }
+  };
+  // bit 4 i + e of `wanted`: slot e of group from + i
+  auto carry = [&](uint32_t wanted, int from) {
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int i = 0; i < NIT; ++i) store(held[i], i, (wanted >> (4 * i)) & 15u);
+    } else {
+#pragma unroll
+      for (int base = 0; base < 8; base += 4) {
+        if (from + base >= its) break;
+        Group g[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          g[i].page = -1;
+          if ((wanted >> (4 * (base + i))) & 15u) load_page(g[i], from + base + i);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_rest(g[i], from + base + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store(g[i], from + base + i, (wanted >> (4 * (base + i))) & 15u);
+      }
+    }
+  };
+  auto flush = [&](int i, uint32_t& wanted) {   // NIT = 0: after every eighth group and the last
+    if constexpr (NIT == 0) {
+      if ((i & 7) == 7 || i == its - 1) {
+        carry(wanted, i & ~7);
+        wanted = 0;
+      }
+    }
+  };
+  // The new length is written by the sequence's last workgroup to get here: lens_out may be the lengths that all of them have read.
+  // Every wave's load of the length has returned before the barriers in front of this, so the count needs no fence of its own
+  // (one of device scope writes the cache back: 256 workgroups took 25.8 us with it, 18.8 without).
+  auto arrive = [&]() {
+    if (threadIdx.x == 0) {
+      if (atomicAdd(&arrived[b], 1) == c.hkv - 1) {
+        arrived[b] = 0;
+        a.lens_out[b] = over ? budget : len;
+      }
+    }
+  };
+  uint32_t wanted = 0;
+  if (!over) {
+    each([&](int i, int j, const uint32_t (&)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) wanted |= j + e < j1 && !in_place ? 1u << (4 * (i & 7) + e) : 0u;
+      flush(i, wanted);
+    });
+    if constexpr (NIT > 0) carry(wanted, 0);
     if (threadIdx.x == 0) a.n_moves[blockIdx.x] = 0;
+    __syncthreads();                            // every wave has read the length
+    arrive();
     return;
   }
-  const bool in_lds = len <= lds_keys;
-  if (in_lds)
-    for (int j = threadIdx.x; j < len; j += kThreads) keys[j] = key_of(a, meta_index(c, b, head, j), seen);
-  auto key_at = [&](int j) { return in_lds ? keys[j] : key_of(a, meta_index(c, b, head, j), seen); };
 
   // the budget-th largest key, and how many of those equal to it stay
   uint32_t prefix = 0;
@@ -124,80 +240,119 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, con
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
     const uint32_t above = pass == 0 ? 0u : (pass == 1 ? 0xFFE00000u : 0xFFFFFC00u);
-    for (int i = threadIdx.x; i < 2048; i += kThreads) hist[i] = 0;
+    *reinterpret_cast<int2*>(&hist[2 * threadIdx.x]) = make_int2(0, 0);
     __syncthreads();
-    for (int j = threadIdx.x; j < len; j += kThreads) {
-      const uint32_t k = key_at(j);
-      if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
-    }
+    each([&](int, int j, const uint32_t (&k)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < j1 && (k[e] & above) == prefix) atomicAdd(&hist[(k[e] >> shift) & (bins - 1)], 1);
+    });
     __syncthreads();
-    // from the largest digit down: thread t has digits bins - 1 - 2 t and the next one
-    const int d0 = 2047 - 2 * (int)threadIdx.x, n0 = hist[d0], n1 = hist[d0 - 1];
+    // from the largest digit down: thread t has digits 2047 - 2 t and the one below
+    const int d0 = 2047 - 2 * (int)threadIdx.x;
+    const int2 n = *reinterpret_cast<const int2*>(&hist[d0 - 1]);
+    const int n0 = n.y, n1 = n.x;
     int upto = n0 + n1;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int x = __shfl_up(upto, o);
       if (lane >= o) upto += x;
     }
-    int total;
-    const int before = before_me(__shfl(upto, 63), wave, sums, total) + upto - n0 - n1;
+    const int before = before_me({__shfl(upto, 63), 0}, wave, sums).x + upto - n0 - n1;
     if (before < want && before + n0 >= want) {
       found[0] = d0;
       found[1] = want - before;
+      found[2] = n0;
     } else if (before + n0 < want && before + n0 + n1 >= want) {
       found[0] = d0 - 1;
       found[1] = want - before - n0;
+      found[2] = n1;
     }
     __syncthreads();
     prefix |= (uint32_t)found[0] << shift;
-    want = found[1];
-    __syncthreads();
+    want = found[1];                            // (read before the next pass's first barrier, written behind its second)
   }
+  const bool ranked = want < found[2];          // not all of the equal ones stay
 
-  // contiguous parts of the slots, a multiple of 64 each
-  const int part = ((len + kThreads - 1) / kThreads) * 64, j0 = min(len, wave * part), j1 = min(len, j0 + part);
-  int ties = 0;
-  for (int j = j0; j < j1; j += 64) ties += __popcll(__ballot(j + lane < j1 && key_at(j + lane) == prefix));
-  int total;
-  const int ties_before = before_me(ties, wave, sums, total);
-  auto walk = [&](auto&& each) {
-    int tie = ties_before;
-    for (int j = j0; j < j1; j += 64) {
-      const bool real = j + lane < j1;
-      const uint32_t k = real ? key_at(j + lane) : 0u;
-      const uint64_t same = __ballot(real && k == prefix);
-      const int rank = tie + __popcll(same & ((1ull << lane) - 1));
-      tie += __popcll(same);
-      const bool stays = real && (k > prefix || (k == prefix && rank < want));
-      each(j + lane, real, stays);
-    }
+  // of a count of 0..4 in every lane: the sum over the lanes below, and over all
+  const uint64_t below = (1ull << lane) - 1;
+  auto lanes_below = [&](int n, int& all) {
+    const uint64_t b0 = __ballot(n & 1), b1 = __ballot(n & 2), b2 = __ballot(n & 4);
+    all = __popcll(b0) + 2 * __popcll(b1) + 4 * __popcll(b2);
+    return __popcll(b0 & below) + 2 * __popcll(b1 & below) + 4 * __popcll(b2 & below);
   };
-  int holes = 0, movers = 0;
-  walk([&](int j, bool real, bool stays) {
-    holes += __popcll(__ballot(real && !stays && j < budget));
-    movers += __popcll(__ballot(stays && j >= budget));
-  });
-  int n_moves;
-  int hole = before_me(holes, wave, sums, n_moves);
-  int mover = before_me(movers, wave, sums, total);
-  walk([&](int j, bool real, bool stays) {
-    const bool is_hole = real && !stays && j < budget, is_mover = stays && j >= budget;
-    const uint64_t hm = __ballot(is_hole), mm = __ballot(is_mover), below = (1ull << lane) - 1;
-    if (is_hole) moves[hole + __popcll(hm & below)].y = j;
-    if (is_mover) moves[mover + __popcll(mm & below)].x = j;
-    hole += __popcll(hm);
-    mover += __popcll(mm);
-    if (real) {
-      const int64_t at = meta_index(c, b, head, j);
-      if (at < 0) {
-        note_bad_page(c);
-      } else if (stays && j < budget) {
-        a.weights_out[at] = c.weights[at];
-        a.ids_out[at] = c.ids[at];
+  int ties_before = 0;
+  if (ranked) {
+    int ties = 0;
+    each([&](int, int j, const uint32_t (&k)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ties += __popcll(__ballot(j + e < j1 && k[e] == prefix));
+    });
+    ties_before = before_me({ties, 0}, wave, sums).x;
+  }
+  // f(group number, first slot, which of the four slots stay (a bit each))
+  auto walk = [&](auto&& f) {
+    int tie = ties_before;
+    each([&](int i, int j, const uint32_t (&k)[4]) {
+      uint32_t stay = 0, same = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        stay |= j + e < j1 && k[e] > prefix ? 1u << e : 0u;
+        same |= j + e < j1 && k[e] == prefix ? 1u << e : 0u;
       }
-    }
+      if (ranked) {
+        int all;
+        int rank = tie + lanes_below(__popc(same), all);
+        tie += all;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((same >> e) & 1) stay |= rank++ < want ? 1u << e : 0u;
+      } else {
+        stay |= same;
+      }
+      f(i, j, stay);
+    });
+  };
+  auto real_of = [&](int j) { return j >= j1 ? 0u : (j1 - j >= 4 ? 15u : (1u << (j1 - j)) - 1u); };
+  auto in_budget = [&](int j) { return j >= budget ? 0u : (budget - j >= 4 ? 15u : (1u << (budget - j)) - 1u); };
+  int holes = 0, movers = 0;                    // of this lane
+  walk([&](int, int j, uint32_t stay) {
+    holes += __popc(real_of(j) & ~stay & in_budget(j));
+    movers += __popc(stay & ~in_budget(j));
   });
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    holes += __shfl_xor(holes, o);
+    movers += __shfl_xor(movers, o);
+  }
+  Counts total;
+  const Counts first = before_me({holes, movers}, wave, sums, &total);
+  const int n_moves = total.x;                  // as many tokens behind the budget stay as tokens before it leave
+  int hole = first.x, mover = first.y;
+  walk([&](int i, int j, uint32_t stay) {
+    const uint32_t lose = real_of(j) & ~stay & in_budget(j), move = stay & ~in_budget(j);
+    if (__ballot(lose != 0)) {
+      int all;
+      int at = hole + lanes_below(__popc(lose), all);
+      hole += all;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((lose >> e) & 1) moves[at++].y = j + e;
+    }
+    if (__ballot(move != 0)) {
+      int all;
+      int at = mover + lanes_below(__popc(move), all);
+      mover += all;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((move >> e) & 1) moves[at++].x = j + e;
+    }
+    wanted |= in_place ? 0u : (stay & in_budget(j)) << (4 * (i & 7));
+    flush(i, wanted);
+  });
+  if constexpr (NIT > 0) carry(wanted, 0);
   if (threadIdx.x == 0) a.n_moves[blockIdx.x] = n_moves;
+  arrive();
   if (!move_here) return;
   __syncthreads();                              // the moves are this workgroup's own
   move_rows<ROW_BYTES>(a, b, head, moves, n_moves, 0, kThreads / (ROW_BYTES / 16));
@@ -215,11 +370,15 @@ __global__ __launch_bounds__(256) void move_kernel(const EvictArgs a, const int 
 
 void launch_evict(const EvictArgs& a, int d, bool e4m3, int32_t* arrived, hipStream_t st) {
   const int jobs = a.c.n_seqs * a.c.hkv;
-  const int lds_keys = a.c.max_len < kLdsKeys ? a.c.max_len : kLdsKeys;
   const bool here = a.max_moves <= kFewMoves;
   auto go = [&](auto rb) {
     constexpr int kRB = decltype(rb)::value;
-    select_kernel<kRB><<<dim3((unsigned)jobs), dim3(kThreads), (size_t)lds_keys * 4, st>>>(a, lds_keys, here, arrived);
+    const dim3 grid((unsigned)jobs), block(kThreads);
+    if (a.c.max_len <= 4 * kThreads) select_kernel<kRB, 1><<<grid, block, 0, st>>>(a, here, arrived);
+    else if (a.c.max_len <= 8 * kThreads) select_kernel<kRB, 2><<<grid, block, 0, st>>>(a, here, arrived);
+    else if (a.c.max_len <= 16 * kThreads) select_kernel<kRB, kHold><<<grid, block, 0, st>>>(a, here, arrived);
+    else if (a.c.max_len <= 32 * kThreads) select_kernel<kRB, 8><<<grid, block, 0, st>>>(a, here, arrived);
+    else select_kernel<kRB, 0><<<grid, block, 0, st>>>(a, here, arrived);
     if (!here) {
       const int rows = 256 / (kRB / 16);
       int parts = (a.max_moves + 4 * rows - 1) / (4 * rows);          // four rows a lane group where every move happens
@@ -231,15 +390,6 @@ void launch_evict(const EvictArgs& a, int d, bool e4m3, int32_t* arrived, hipStr
   if (rb == 256) go(std::integral_constant<int, 256>{});
   else if (rb == 128) go(std::integral_constant<int, 128>{});
   else go(std::integral_constant<int, 64>{});
-}
-
-hipError_t prepare_evict() {
-  // 128 KB of keys are more than a workgroup gets unasked
-  for (const void* f : {(const void*)select_kernel<256>, (const void*)select_kernel<128>, (const void*)select_kernel<64>}) {
-    const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsKeys * 4);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
 }
 
 }  // namespace paged

@@ -60,7 +60,6 @@ void launch_evict(const EvictArgs& a, int, bool, int32_t* arrived, hipStream_t) 
   a.moves[0] = a.moves[jobs * a.max_moves - 1] = int2{1, 1};
   for (int i = 0; i < a.c.n_seqs; ++i) CHECK(arrived[i] == 0);
 }
-hipError_t prepare_evict() { return hipSuccess; }
 }  // namespace paged
 }  // namespace kvx
 
@@ -224,6 +223,10 @@ void refusals() {
   REFUSED(KV_E_INVAL, kAll, a.p.page_stride = -2048);
   REFUSED(KV_E_INVAL, kAll, a.p.page_stride = 1ll << 41);
   REFUSED(KV_E_INVAL, kAll, a.p.k_scale = (float*)1);
+  REFUSED(KV_E_INVAL, kAll, a.p.weights += 1);
+  REFUSED(KV_E_INVAL, kAll, a.p.ids += 2);
+  REFUSED(KV_E_INVAL, kAttend | kEvict, w += 1);
+  REFUSED(KV_E_INVAL, kEvict, ids_out += 1);
   REFUSED(KV_E_INVAL, kAppend, po = nullptr);
   REFUSED(KV_E_INVAL, kAppend, pq = nullptr);
   REFUSED(KV_E_INVAL, kAppend, q_out.tok_stride += 8);
