@@ -31,6 +31,8 @@ struct kv_paged {
   float* lse = nullptr;         // [max_tokens][Hq], where the caller wants weights but no lse
   uint8_t* work = nullptr;      // partial results of an attention launch, or the moves of an eviction: calls are ordered
   int64_t part_rows_cap = 0;    // rows of partial results that fit
+  float* logits = nullptr;      // of launches of few rows that collect weights
+  int64_t logits_cap = 0;       // floats
   std::string err;
 };
 
@@ -279,9 +281,12 @@ int kv_paged_init(const kv_paged_config* cfg, kv_paged** out) {
   h->part_rows_cap = std::min<int64_t>(1 << 18, std::max(few_rows, chunk_rows) * ((c.max_len + 127) / 128));
   const int64_t part_bytes = h->part_rows_cap * (c.head_dim * 4 + 8);
   const int64_t move_bytes = (int64_t)c.max_seqs * c.n_kv_heads * ((int64_t)c.max_evicted * 8 + 4);
+  // logits: for the largest such launch, up to 128 MB (calls that would need more form them twice)
+  h->logits_cap = std::min<int64_t>(1 << 25, few_rows * align_up(c.max_len, 64));
   const int64_t head_bytes = align_up(256 + 64 * 8 + (int64_t)c.max_seqs * 4, 256);
   const int64_t lse_bytes = align_up((int64_t)c.max_tokens * c.n_q_heads * 4, 256);
-  const int64_t bytes = head_bytes + lse_bytes + align_up(std::max(part_bytes, move_bytes), 256);
+  const int64_t logit_bytes = align_up(h->logits_cap * 4, 256);
+  const int64_t bytes = head_bytes + lse_bytes + logit_bytes + align_up(std::max(part_bytes, move_bytes), 256);
   e = hipMalloc((void**)&h->mem, (size_t)bytes);
   if (e != hipSuccess) {
     rc = fail(nullptr, e == hipErrorOutOfMemory ? KV_E_NOMEM : KV_E_HIP, "kv_paged_init: device allocation of %lld bytes failed: %s", (long long)bytes,
@@ -295,7 +300,8 @@ int kv_paged_init(const kv_paged_config* cfg, kv_paged** out) {
   h->turns = (uint64_t*)(h->mem + 256);
   h->arrived = (int32_t*)(h->mem + 256 + 64 * 8);
   h->lse = (float*)(h->mem + head_bytes);
-  h->work = h->mem + head_bytes + lse_bytes;
+  h->logits = (float*)(h->mem + head_bytes + lse_bytes);
+  h->work = h->mem + head_bytes + lse_bytes + logit_bytes;
   uint8_t* head = new (std::nothrow) uint8_t[(size_t)head_bytes];
   if (!head) {
     kv_paged_destroy(h);
@@ -366,12 +372,18 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
     plan_tiles(h, a, tile_rows);
     plan_splits(h, a, tile_rows == kFewRows);
     if ((int64_t)a.tiles * a.c.hkv * a.splits > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: too many workgroups");
+    // A kept logit is 4 bytes written and 4 read, a key formed again d elements: up to as many rows as make that the same.
+    a.logit_stride = align_up(a.c.max_len, 64);
+    if (weights_out && tile_rows == kFewRows && 8ll * a.part_rows <= (int64_t)c.head_dim * h->cache_elt &&
+        (int64_t)a.tiles * a.c.hkv * a.part_rows * a.logit_stride <= h->logits_cap)
+      a.logits = h->logits;
     a.part_o = (float*)h->work;
     a.part_ml = (float2*)(h->work + h->part_rows_cap * c.head_dim * 4);
     launch_attend(a, c.head_dim, c.dtype, e4m3, tile_rows, st);
     if (a.splits > 1) launch_merge(a, c.head_dim, c.dtype, tile_rows, e4m3, st);
   }
-  if (weights_out) launch_weights(a, c.head_dim, c.dtype, e4m3, st);
+  if (a.logits) launch_weights_from_logits(a, st);
+  else if (weights_out) launch_weights(a, c.head_dim, c.dtype, e4m3, st);
   return launched(h, "kv_paged_attend");
 }
 

@@ -84,6 +84,10 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     }
   };
 
+  // where this lane's row keeps its logits: the keys of half h, four at a time
+  float* const logits = a.logits && (lane & 31) < n_rows
+                            ? a.logits + (((int64_t)tile * c.hkv + head) * a.part_rows + (lane & 31)) * a.logit_stride + 4 * h : nullptr;
+
   int u = k0 + 32 * wave;
   if (u < k1) {
     fetch_page(u);
@@ -109,6 +113,11 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     }
     f32x16 x = w.logits(lk, lane);
     if (u + 32 > all_hi || u < all_lo || absent) w.mask(x, u, absent, h);
+    if (logits)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(logits + u + 8 * g) =
+            make_float4(x[4 * g] * factor, x[4 * g + 1] * factor, x[4 * g + 2] * factor, x[4 * g + 3] * factor);
     w.soften(x, factor);
 #pragma unroll
     for (int r = 0; r < 16; ++r) w.l += x[r];

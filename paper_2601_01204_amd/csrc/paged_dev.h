@@ -50,6 +50,8 @@ struct AttendArgs {
   float2* part_ml;
   const float* weights_in;
   float* weights_out;
+  float* logits;                // launches of few rows that collect weights: [tile][key head][row][logit_stride], log2 units; NULL: not kept
+  int64_t logit_stride;
   float factor;                 // softmax scale * log2(e)
   int32_t causal, window;
   int32_t tiles;                // row tiles of the launch (all sequences), per key head and split
@@ -74,6 +76,7 @@ struct EvictArgs {
 void launch_append(const AppendArgs& a, int d, int dtype, bool e4m3, bool interleaved, hipStream_t st);
 void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_rows, hipStream_t st);
 void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m3, hipStream_t st);
+void launch_weights_from_logits(const AttendArgs& a, hipStream_t st);
 void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st);
 // arrived: [n_seqs], zero before and after
 void launch_evict(const EvictArgs& a, int d, bool e4m3, int32_t* arrived, hipStream_t st);

@@ -1,7 +1,10 @@
 // Weights that cached tokens receive in a call's attention: weights_out_j = weights_j + sum over the call's rows of the key head's group
 // of softmax weight (row, j), from the rows' lse.
 //
-// A workgroup owns 128 keys of one key head, a wave 32 of them, whose fragments stay in registers, and goes over all rows that see
+// weights_from_logits_kernel, behind attention launches of few rows, reads the logits that those kept: 8 bytes a row and key, written and
+// read, where K would be another d elements.  weights_kernel forms them again.
+//
+// weights_kernel.  A workgroup owns 128 keys of one key head, a wave 32 of them, whose fragments stay in registers, and goes over all rows that see
 // them, 32 at a time, brought into LDS for the four waves.  S = Q K^T with a key in a lane and its rows in that lane's registers: a key's
 // weights are summed in its lane, in row order, in fp32 without a rounding between, and no two workgroups write the same
 // token, so the sums do not depend on what ran when.
@@ -131,7 +134,64 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   }
 }
 
+// A thread has four neighbouring keys of one key head.  A row's range of keys (row tiles of decoding see them all but for masks) was
+// written as far as its tile goes; keys that no row of the tile read (in front of a window) have no logits and gain nothing.
+template <int kThreads>
+__global__ __launch_bounds__(kThreads) void weights_from_logits_kernel(const AttendArgs a) {
+  const Call& c = a.c;
+  __shared__ float lse[32];
+  const int key_blocks = (c.max_len + 4 * kThreads - 1) / (4 * kThreads);
+  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
+  const int block = rest % key_blocks, b = rest / key_blocks;
+  const Seq s = sequence(c, b);
+  if (block * 4 * kThreads >= s.len) return;
+  const int rows = s.n * c.group;                            // one tile of a sequence's rows
+  if ((int)threadIdx.x < rows) {
+    const int it = threadIdx.x / c.group, g = threadIdx.x - it * c.group;
+    const float x = a.lse[(int64_t)(s.first + it) * c.hq + head * c.group + g];
+    lse[threadIdx.x] = x == -kInf ? kInf : x * 1.4426950408889634f;
+  }
+  __syncthreads();
+  const int key = (block * kThreads + threadIdx.x) * 4;
+  if (key >= s.len) return;
+  const int32_t page = page_of(c, b, key >> c.page_shift);
+  if (page < 0) {
+    note_bad_page(c);
+    return;
+  }
+  const int64_t at = (((int64_t)page * c.hkv + head) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+  const float4 before = *reinterpret_cast<const float4*>(a.weights_in + at);
+  const Range range = rows ? tile_range(a, s, 0, rows) : Range{0, 0};
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  if (key >= range.lo && key < range.hi) {
+    const float* x = a.logits + ((int64_t)b * c.hkv + head) * a.part_rows * a.logit_stride + key;
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+      const float4 y = *reinterpret_cast<const float4*>(x + r * a.logit_stride);
+      sum[0] += __builtin_amdgcn_exp2f(y.x - lse[r]);
+      sum[1] += __builtin_amdgcn_exp2f(y.y - lse[r]);
+      sum[2] += __builtin_amdgcn_exp2f(y.z - lse[r]);
+      sum[3] += __builtin_amdgcn_exp2f(y.w - lse[r]);
+    }
+  }
+  float* out = a.weights_out + at;
+  const float w[4] = {before.x + sum[0], before.y + sum[1], before.z + sum[2], before.w + sum[3]};
+  if (key + 4 <= s.len) {
+    *reinterpret_cast<float4*>(out) = make_float4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (key + e < s.len) out[e] = w[e];
+  }
+}
+
 }  // namespace
+
+void launch_weights_from_logits(const AttendArgs& a, hipStream_t st) {
+  constexpr int kThreads = 256;
+  const dim3 grid((unsigned)((int64_t)((a.c.max_len + 4 * kThreads - 1) / (4 * kThreads)) * a.c.hkv * a.c.n_seqs));
+  weights_from_logits_kernel<kThreads><<<grid, dim3(kThreads), 0, st>>>(a);
+}
 
 void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)((a.c.max_len + kKeys - 1) / kKeys) * a.c.hkv * a.c.n_seqs));

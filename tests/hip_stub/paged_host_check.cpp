@@ -52,6 +52,12 @@ void launch_weights(const AttendArgs& a, int, int, bool, hipStream_t) {
   CHECK(a.lse && a.weights_in && a.weights_out);
   if (a.c.n_tokens) a.lse[(int64_t)a.c.n_tokens * a.c.hq - 1] = 1.f;
 }
+void launch_weights_from_logits(const AttendArgs& a, hipStream_t) {
+  ++weighings;
+  CHECK(last_rows == 32 && a.tiles_per_seq == 1 && a.lse && a.weights_in && a.weights_out && a.logit_stride >= a.c.max_len);
+  CHECK(a.logit_stride % 4 == 0 && (int64_t)a.c.max_new * a.c.group <= a.part_rows);
+  a.logits[0] = a.logits[(int64_t)a.tiles * a.c.hkv * a.part_rows * a.logit_stride - 1] = 1.f;
+}
 void launch_evict(const EvictArgs& a, int, bool, int32_t* arrived, hipStream_t) {
   ++evictions;
   const int64_t jobs = (int64_t)a.c.n_seqs * a.c.hkv;
@@ -132,9 +138,13 @@ void plans() {
     std::vector<float> w(4);
     p.weights = w.data();
     CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.q, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
+    a.b.n_tokens = std::min(c.max_tokens, c.max_seqs);
+    a.b.n_seqs = c.max_seqs;
+    a.b.max_new = 1;
+    CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.q, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
     kv_paged_destroy(h);
   }
-  CHECK(attends > 18000 && merges > 1000 && evictions > 1000 && weighings == 3000);
+  CHECK(attends > 18000 && merges > 1000 && evictions > 1000 && weighings == 6000);
 }
 
 void frequencies() {
