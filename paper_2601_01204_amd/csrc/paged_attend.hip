@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      rk[i] = *reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride);
-      rv[i] = *reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride);
+      rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride));
+      rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride));
     }
   };
 
