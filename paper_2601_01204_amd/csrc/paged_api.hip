@@ -209,28 +209,38 @@ void plan_tiles(const kv_paged* h, AttendArgs& a, int tile_rows) {
   a.part_rows = (int32_t)std::min<int64_t>(tile_rows, (int64_t)a.c.max_new * h->group);
 }
 
-// Key ranges per row tile.
-void plan_splits(const kv_paged* h, AttendArgs& a, bool few) {
+// Most keys that a row tile reads.
+int64_t reach(const AttendArgs& a) {
   int64_t keys = a.c.max_len;
   if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + (a.causal ? std::min<int64_t>(a.c.max_new, kChunkRows) : a.c.max_new) + 64);
-  keys = align_up(keys, 64);
-  const int64_t columns = (int64_t)a.tiles * a.c.hkv;
+  return align_up(keys, 64);
+}
+
+// Launches of few rows: as many workers as the chip holds workgroups of that kernel (by its LDS and registers two on a compute unit
+// where a row of d channels is 256 bytes or its outputs are, three else).  Short columns, or many that are not long, have a workgroup each
+// and nothing to join.
+int few_workers(const kv_paged* h) { return (h->cfg.head_dim == 128 ? 2 : 3) * h->n_cus; }
+void plan_workers(const kv_paged* h, AttendArgs& a) {
+  const int64_t keys = reach(a), columns = (int64_t)a.tiles * a.c.hkv;
+  const int workers = few_workers(h);
+  a.splits = 1;
+  a.split_keys = (int32_t)keys;
+  a.workers = keys <= 256 || (keys <= 1024 && columns >= 2 * workers) ? 0 : (int32_t)std::min<int64_t>(workers, columns * ((keys + 127) / 128));
+}
+
+// Launches of more rows: key ranges per row tile, for the fewest rounds of two workgroups a compute unit; a workgroup costs about four
+// tiles of 64 keys by itself.
+void plan_splits(const kv_paged* h, AttendArgs& a) {
+  const int64_t keys = reach(a), columns = (int64_t)a.tiles * a.c.hkv;
   const int64_t fit = std::max<int64_t>(1, h->part_rows_cap / std::max<int64_t>(1, columns * a.part_rows));
+  const int64_t slots = 2ll * h->n_cus, tiles = keys / 64;
   int64_t range = keys;
-  if (few) {
-    // ranges short enough to fill the chip several times over (sequences differ in length), no shorter than a unit of each wave
-    const int64_t want = std::max<int64_t>(1, 16ll * h->n_cus / columns);
-    if (keys > 1024 || columns < 2 * h->n_cus) range = std::max<int64_t>(128, align_up((keys + want - 1) / want, 128));
-  } else {
-    // rounds of two workgroups a compute unit; a workgroup costs about four tiles of 64 keys by itself
-    const int64_t slots = 2ll * h->n_cus, tiles = keys / 64;
-    double best = 0.0;
-    for (int64_t s = 1; s <= std::min<int64_t>(16, tiles); ++s) {
-      const double cost = (double)((columns * s + slots - 1) / slots) * ((double)((tiles + s - 1) / s) + 4.0) + (s > 1 ? 4.0 : 0.0);
-      if (s == 1 || cost < 0.97 * best) {
-        best = cost;
-        range = (tiles + s - 1) / s * 64;
-      }
+  double best = 0.0;
+  for (int64_t s = 1; s <= std::min<int64_t>(16, tiles); ++s) {
+    const double cost = (double)((columns * s + slots - 1) / slots) * ((double)((tiles + s - 1) / s) + 4.0) + (s > 1 ? 4.0 : 0.0);
+    if (s == 1 || cost < 0.97 * best) {
+      best = cost;
+      range = (tiles + s - 1) / s * 64;
     }
   }
   int64_t splits = (keys + range - 1) / range;
@@ -274,11 +284,12 @@ int kv_paged_init(const kv_paged_config* cfg, kv_paged** out) {
   }
   h->n_cus = cus;
 
-  // partial results: what the plans of plan_splits can ask for, up to 256 K rows of them (calls that would need more get fewer ranges)
+  // partial results: two places a worker, and what plan_splits can ask for up to 256 K rows (calls that would need more get fewer ranges)
   const int64_t few_rows = (int64_t)c.n_kv_heads * c.max_seqs * std::min<int64_t>(kFewRows, (int64_t)c.max_tokens * h->group);
   const int64_t chunk_rows = (int64_t)c.max_tokens * h->group > kFewRows
                                  ? c.n_kv_heads * ((int64_t)c.max_tokens * h->group + (int64_t)kChunkRows * c.max_seqs) : 0;
-  h->part_rows_cap = std::min<int64_t>(1 << 18, std::max(few_rows, chunk_rows) * ((c.max_len + 127) / 128));
+  h->part_rows_cap = std::max<int64_t>(2ll * few_workers(h) * std::min<int64_t>(kFewRows, (int64_t)c.max_tokens * h->group),
+                                       std::min<int64_t>(1 << 18, chunk_rows * ((c.max_len + 127) / 128)));
   const int64_t part_bytes = h->part_rows_cap * (c.head_dim * 4 + 8);
   const int64_t move_bytes = (int64_t)c.max_seqs * c.n_kv_heads * ((int64_t)c.max_evicted * 8 + 4);
   // logits: for the largest such launch, up to 128 MB (calls that would need more form them twice)
@@ -370,7 +381,8 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
     const int64_t rows = (int64_t)a.c.max_new * h->group;
     const int tile_rows = rows <= kFewRows ? kFewRows : kChunkRows;
     plan_tiles(h, a, tile_rows);
-    plan_splits(h, a, tile_rows == kFewRows);
+    if (tile_rows == kFewRows) plan_workers(h, a);
+    else plan_splits(h, a);
     if ((int64_t)a.tiles * a.c.hkv * a.splits > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: too many workgroups");
     // A kept logit is 4 bytes written and 4 read, a key formed again d elements: up to as many rows as make that the same.
     a.logit_stride = align_up(a.c.max_len, 64);
@@ -380,7 +392,7 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
     a.part_o = (float*)h->work;
     a.part_ml = (float2*)(h->work + h->part_rows_cap * c.head_dim * 4);
     launch_attend(a, c.head_dim, c.dtype, e4m3, tile_rows, st);
-    if (a.splits > 1) launch_merge(a, c.head_dim, c.dtype, tile_rows, e4m3, st);
+    if (a.splits > 1 || a.workers) launch_merge(a, c.head_dim, c.dtype, tile_rows, e4m3, st);
   }
   if (a.logits) launch_weights_from_logits(a, st);
   else if (weights_out) launch_weights(a, c.head_dim, c.dtype, e4m3, st);

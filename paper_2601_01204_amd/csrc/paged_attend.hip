@@ -21,175 +21,175 @@ __device__ __forceinline__ void store_out(const AttendArgs& a, int token, int he
 }
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
-// ---- up to 32 rows: four waves, each with a ring of units of its own -------------------------------------------
-// Bound by memory: every key and value is read once.  A wave works on every fourth unit of the range, brings it through registers into
-// its own part of LDS and holds the next unit's loads in flight meanwhile (16 KB a wave, 8 waves a compute unit); no wave waits
+// ---- up to 32 rows: four waves, each with units of its own --------------------------------------------------------
+// Bound by memory: every key and value is read once, past the caches.  A wave works on every fourth 32 keys, brings them through
+// registers into its own part of LDS and holds the next loads in flight meanwhile (16 KB a wave, 8 waves a compute unit); no wave waits
 // for another before the end, where the four waves' statistics and outputs are joined through the same LDS.
-template <typename T, int D, bool E4M3>
+//
+// A workgroup costs some 5 us besides its keys, so as many as the chip holds at a time (workers) share the keys of all columns evenly,
+// whatever the sequences' lengths: a worker's share ends inside a column, and merge_kernel joins the pieces.  Against ranges of
+// equal length, several to a slot, us: 64 sequences of up to 8192 tokens 207 -> 186, four of 131072 in 8 bits 215 -> 175.
+template <typename T, int D, bool E4M3, int ROWS>
 __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) {
   typedef Shape<D, E4M3> S;
+  typedef FewRows<T, D, E4M3, ROWS> W;
   constexpr int kRB = S::kRowBytes, kLPR = S::kLanesPerRow;
   constexpr int kLoads = 32 * kLPR / 64;                     // 16-byte loads of a lane for 32 rows
   constexpr int kWaveBytes = 64 * kRB;
-  constexpr int kJoinBytes = 32 * D * 4;
+  constexpr int kJoinBytes = ROWS * D * 4;
   __shared__ __align__(16) uint8_t lds[4 * (kWaveBytes > kJoinBytes ? kWaveBytes : kJoinBytes)];
-  __shared__ float2 stats[4][32];
+  __shared__ float2 stats[4][ROWS];
 
   const Call& c = a.c;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
-  const int split = rest % a.splits, tile = rest / a.splits;
-  int b, t;
-  if (!find_tile(a, tile, 32, b, t)) return;
-  const Seq s = sequence(c, b);
-  const int rows = s.n * c.group, row0 = t * 32;
-  if (row0 >= rows) return;
-  const int n_rows = min(32, rows - row0);
-  const Range range = tile_range(a, s, row0, n_rows);
-  const int n_splits = splits_of(a, range);
-  if (split >= n_splits) return;
-  const int k0 = range.lo + split * a.split_keys, k1 = split_end(a, range, split);
-
-  RowBlock<T, D, E4M3> w;
-  w.clear();
-  const int row = row0 + min(lane & 31, n_rows - 1);         // lanes without a row repeat the last one's
-  const int i_row = row / c.group, g_row = row - i_row * c.group;
-  const int place = s.len - s.n + i_row;
-  w.hi = a.causal ? min(s.len, place + 1) : s.len;
-  w.lo = a.window > 0 ? place + 1 - a.window : 0;
-  w.load_queries(a.q.p + (int64_t)(s.first + i_row) * a.q.tok + (int64_t)(head * c.group + g_row) * a.q.head, h);
-  // keys [all_lo, all_hi) are seen by every row
-  const int all_hi = a.causal ? min(s.len, s.len - s.n + row0 / c.group + 1) : s.len;
-  const int all_lo = a.window > 0 ? s.len - s.n + (row0 + n_rows - 1) / c.group + 1 - a.window : 0;
-  const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
-
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), my_row = lane % ROWS, j = lane / ROWS;
   uint8_t* const lk = lds + wave * kWaveBytes;
   uint8_t* const lv = lk + 32 * kRB;
   const int ld_row = lane / kLPR * kLoads, ld_chunk = lane % kLPR;
-  const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
-  const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
-  u32x4 rk[kLoads], rv[kLoads];
-  uint32_t absent_next = 0;
-  int32_t page = -1;
-  auto fetch_page = [&](int u) { page = u < k1 ? page_of_key(c, b, u + (lane & 31), s.len) : 0; };
-  auto fetch_rows = [&](int u) {                             // needs fetch_page(u)
-    const uint64_t bad = __ballot(page < 0);
-    absent_next = (uint32_t)bad;
-    if (bad && lane == 0) note_bad_page(c);
-    const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride));
-      rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride));
-    }
-  };
 
-  // where this lane's row keeps its logits: the keys of half h, four at a time
-  float* const logits = a.logits && (lane & 31) < n_rows
-                            ? a.logits + (((int64_t)tile * c.hkv + head) * a.part_rows + (lane & 31)) * a.logit_stride + 4 * h : nullptr;
-
-  int u = k0 + 32 * wave;
-  if (u < k1) {
-    fetch_page(u);
-    fetch_rows(u);
-    fetch_page(u + 128);
+  int unit = 0, unit_end = 1;                                // this workgroup's units; without workers: one column, whatever it holds
+  if (a.workers) {
+    const int total = units_before(a, c.n_seqs) * c.hkv, share = share_of(a, total);
+    unit = blockIdx.x * share;
+    unit_end = min(total, unit + share);
   }
-  for (; u < k1; u += 128) {
-    const uint32_t absent = absent_next;
-    // values behind the end and without a page are zero: a probability of zero times what lies there would not be
-    const bool tail = u + 32 > s.len || absent;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = ld_row + i;
-      if (tail && (u + r >= s.len || ((absent >> r) & 1))) rv[i] = (u32x4){0, 0, 0, 0};
-      *reinterpret_cast<u32x4*>(lk + lds_offset<kRB>(r, ld_chunk)) = rk[i];
-      *reinterpret_cast<u32x4*>(lv + lds_offset<kRB>(r, ld_chunk)) = rv[i];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // this wave's LDS only: its accesses are carried out in order
-    __builtin_amdgcn_wave_barrier();
-    if (u + 128 < k1) {
-      fetch_rows(u + 128);
-      fetch_page(u + 256);
-    }
-    f32x16 x = w.logits(lk, lane);
-    if (u + 32 > all_hi || u < all_lo || absent) w.mask(x, u, absent, h);
-    if (logits)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(logits + u + 8 * g) =
-            make_float4(x[4 * g] * factor, x[4 * g + 1] * factor, x[4 * g + 2] * factor, x[4 * g + 3] * factor);
-    w.soften(x, factor);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) w.l += x[r];
-    // probabilities as a pair of 16-bit values, so that they are not rounded before the output is (the matrix cores have time)
-#pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      u32x4 p, p_low;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x0 = x[8 * st + 2 * e], x1 = x[8 * st + 2 * e + 1];
-        p[e] = T::pack(x0, x1);
-        p_low[e] = T::pack(x0 - T::low(p[e]), x1 - T::high(p[e]));
-      }
-#pragma unroll
-      for (int cb = 0; cb < S::kBlocks; ++cb) {
-        const u32x4 f = w.value_fragment(lv, lane, st, cb);
-        w.o[cb] = T::mfma(f, p, w.o[cb]);
-        w.o[cb] = T::mfma(f, p_low, w.o[cb]);
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-
-  // join the four waves
-  {
-    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
-    w.l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
-  }
-  if (h == 0) stats[wave][lane] = make_float2(w.m, w.l);
-  __syncthreads();                                           // (also: no wave reads its K and V any more)
-  float m = -kInf;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m = fmaxf(m, stats[i][lane & 31].x);
-  const float mine = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
-  float* const jo = reinterpret_cast<float*>(lds) + wave * 32 * D;
-#pragma unroll
-  for (int cb = 0; cb < S::kBlocks; ++cb)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) jo[(lane & 31) * D + ((32 * cb + 8 * g + 4 * h + e) ^ (4 * (lane & 7)))] = w.o[cb][4 * g + e] * mine;
-  __syncthreads();
-  const float v_scale = E4M3 && c.v_scale ? c.v_scale[head] : 1.f;
-  const int64_t block = ((int64_t)tile * c.hkv + head) * a.splits + split;
-  for (int at = threadIdx.x; at < n_rows * (D / 4); at += 256) {
-    const int r = at / (D / 4), ch = at % (D / 4) * 4;
-    float top = -kInf, sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, stats[i][r].x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum += top == -kInf ? 0.f : stats[i][r].y * __builtin_amdgcn_exp2f(stats[i][r].x - top);
-    float o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds) + (i * 32 + r) * D + (ch ^ (4 * (r & 7))));
-      o[0] += x.x;
-      o[1] += x.y;
-      o[2] += x.z;
-      o[3] += x.w;
-    }
-    const int row_r = row0 + r, i_r = row_r / c.group, token = s.first + i_r, qh = head * c.group + row_r - i_r * c.group;
-    if (n_splits == 1) {
-      const float f = sum == 0.f ? 0.f : v_scale / sum;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] *= f;
-      store_out<T>(a, token, qh, ch, o);
-      if (a.lse && ch == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(top, sum);
+  while (unit < unit_end) {
+    Column col;
+    if (a.workers) {
+      col = column_of(a, unit);
     } else {
-      *reinterpret_cast<float4*>(a.part_o + (block * a.part_rows + r) * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
-      if (ch == 0) a.part_ml[block * a.part_rows + r] = make_float2(top, sum);
+      col.b = blockIdx.x / c.hkv;
+      col.head = blockIdx.x - col.b * c.hkv;
+      col.first = 0;
+      col.units = 1;
     }
+    const int b = col.b, head = col.head;
+    const Seq s = sequence(c, b);
+    const int n_rows = s.n * c.group;
+    if (n_rows == 0) return;                                 // (a column of a worker has rows)
+    const Range range = tile_range(a, s, 0, n_rows);
+    const int upto = min(unit_end, col.first + col.units);
+    const bool whole = unit == col.first && upto == col.first + col.units;
+    const int k0 = a.workers ? range.lo + (unit - col.first) * kFewKeys : range.lo;
+    const int k1 = a.workers ? min(range.hi, range.lo + (upto - col.first) * kFewKeys) : range.hi;
+
+    W w;
+    w.clear();
+    const int row = min(my_row, n_rows - 1);                 // lanes without a row repeat the last one's
+    const int i_row = row / c.group, g_row = row - i_row * c.group;
+    const int place = s.len - s.n + i_row;
+    w.hi = a.causal ? min(s.len, place + 1) : s.len;
+    w.lo = a.window > 0 ? place + 1 - a.window : 0;
+    w.load_queries(a.q.p + (int64_t)(s.first + i_row) * a.q.tok + (int64_t)(head * c.group + g_row) * a.q.head, j);
+    // keys [all_lo, all_hi) are seen by every row
+    const int all_hi = a.causal ? min(s.len, s.len - s.n + 1) : s.len;
+    const int all_lo = a.window > 0 ? s.len - a.window : 0;
+    const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
+
+    const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
+    const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
+    u32x4 rk[kLoads], rv[kLoads];
+    uint32_t absent_next = 0;
+    int32_t page = -1;
+    auto fetch_page = [&](int u) { page = u < k1 ? page_of_key(c, b, u + (lane & 31), s.len) : 0; };
+    auto fetch_rows = [&](int u) {                           // needs fetch_page(u)
+      const uint64_t bad = __ballot(page < 0);
+      absent_next = (uint32_t)bad;
+      if (bad && lane == 0) note_bad_page(c);
+      const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride));
+        rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride));
+      }
+    };
+    // where this lane's row keeps its logits, four keys at a time
+    float* const logits = a.logits && my_row < n_rows
+                              ? a.logits + (((int64_t)b * c.hkv + head) * a.part_rows + my_row) * a.logit_stride + 4 * j : nullptr;
+
+    int u = k0 + 32 * wave;
+    if (u < k1) {
+      fetch_page(u);
+      fetch_rows(u);
+      fetch_page(u + 128);
+    }
+    for (; u < k1; u += 128) {
+      const uint32_t absent = absent_next;
+      // values behind the end and without a page are zero: a probability of zero times what lies there would not be
+      const bool tail = u + 32 > s.len || absent;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = ld_row + i;
+        if (tail && (u + r >= s.len || ((absent >> r) & 1))) rv[i] = (u32x4){0, 0, 0, 0};
+        *reinterpret_cast<u32x4*>(lk + lds_offset<kRB>(r, ld_chunk)) = rk[i];
+        *reinterpret_cast<u32x4*>(lv + lds_offset<kRB>(r, ld_chunk)) = rv[i];
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // this wave's LDS only: its accesses are carried out in order
+      __builtin_amdgcn_wave_barrier();
+      if (u + 128 < k1) {
+        fetch_rows(u + 128);
+        fetch_page(u + 256);
+      }
+      float x[W::kLogits];
+      w.logits(lk, lane, x);
+      if (u + 32 > all_hi || u < all_lo || absent) w.mask(x, u, absent, j);
+      if (logits)
+#pragma unroll
+        for (int g = 0; g < W::kLogits / 4; ++g)
+          *reinterpret_cast<float4*>(logits + u + W::kSpan * g) =
+              make_float4(x[4 * g] * factor, x[4 * g + 1] * factor, x[4 * g + 2] * factor, x[4 * g + 3] * factor);
+      w.soften(x, factor);
+      w.add_values(x, lv, lane);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+
+    // join the four waves
+    w.l = W::over_row(w.l, [](float x, float y) { return x + y; });
+    if (j == 0) stats[wave][my_row] = make_float2(w.m, w.l);
+    __syncthreads();                                         // (also: no wave reads its K and V any more)
+    float m = -kInf;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(m, stats[i][my_row].x);
+    const float mine = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
+    float* const jo = reinterpret_cast<float*>(lds) + (wave * ROWS + my_row) * D;
+    if (my_row < n_rows)
+#pragma unroll
+      for (int i = 0; i < W::kQuads; ++i)
+        *reinterpret_cast<float4*>(jo + ((W::kSpan * i + 4 * j) ^ (4 * (my_row & 7)))) =
+            make_float4(w.quad(i, 0) * mine, w.quad(i, 1) * mine, w.quad(i, 2) * mine, w.quad(i, 3) * mine);
+    __syncthreads();
+    const float v_scale = E4M3 && c.v_scale ? c.v_scale[head] : 1.f;
+    const int64_t part = ((int64_t)blockIdx.x * 2 + (unit == col.first ? 1 : 0)) * a.part_rows;
+    for (int at = threadIdx.x; at < n_rows * (D / 4); at += 256) {
+      const int r = at / (D / 4), ch = at % (D / 4) * 4;
+      float top = -kInf, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, stats[i][r].x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += top == -kInf ? 0.f : stats[i][r].y * __builtin_amdgcn_exp2f(stats[i][r].x - top);
+      float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds) + (i * ROWS + r) * D + (ch ^ (4 * (r & 7))));
+        o[0] += x.x;
+        o[1] += x.y;
+        o[2] += x.z;
+        o[3] += x.w;
+      }
+      const int i_r = r / c.group, token = s.first + i_r, qh = head * c.group + r - i_r * c.group;
+      if (whole) {
+        const float f = sum == 0.f ? 0.f : v_scale / sum;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= f;
+        store_out<T>(a, token, qh, ch, o);
+        if (a.lse && ch == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(top, sum);
+      } else {
+        *reinterpret_cast<float4*>(a.part_o + (part + r) * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
+        if (ch == 0) a.part_ml[part + r] = make_float2(top, sum);
+      }
+    }
+    unit = upto;
+    if (unit < unit_end) __syncthreads();                    // the next column's keys go where the outputs were joined
   }
 }
 
@@ -349,15 +349,25 @@ __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const in
   const Seq s = sequence(c, b);
   const int i_row = token - s.first;
   if (i_row < 0 || i_row >= s.n) return;
-  const int head = qh / c.group, row = i_row * c.group + qh - head * c.group, t = row / tile_rows, row0 = t * tile_rows;
-  const Range range = tile_range(a, s, row0, min(tile_rows, s.n * c.group - row0));
-  const int n = splits_of(a, range);
+  const int head = qh / c.group, row = i_row * c.group + qh - head * c.group;
+  int64_t first;                                             // the first piece's place among the pieces of part_rows rows each
+  int n, apart = 1;                                          // and from one to the next
+  if (a.workers) {
+    // a worker's places: 0 for a column that began before it, 1 for one that ends behind it, so the first piece lies in a 1, others in a 0
+    const int units = units_of(a, b), before = units_before(a, b) * c.hkv + head * units, share = share_of(a, units_before(a, c.n_seqs) * c.hkv);
+    const int w0 = before / share;
+    n = units ? (before + units - 1) / share - w0 + 1 : 0;
+    first = (int64_t)w0 * 2;
+    apart = 2;
+  } else {
+    const int t = row / tile_rows, row0 = t * tile_rows;
+    n = splits_of(a, tile_range(a, s, row0, min(tile_rows, s.n * c.group - row0)));
+    first = ((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits;
+  }
   if (n == 1) return;                                        // written already
-  const int64_t first = (((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits) * a.part_rows + row - row0;
-  const float2* const ml = a.part_ml + first;
-  const float* const part = a.part_o + first * D;
+  auto piece = [&](int i) { return (first + (int64_t)i * apart + (apart == 2 && i == 0 ? 1 : 0)) * a.part_rows + row % tile_rows; };
   float m = -kInf;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, ml[(int64_t)i * a.part_rows].x);
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, a.part_ml[piece(i)].x);
 #pragma unroll
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   const float ref = m == -kInf ? 0.f : m;
@@ -365,8 +375,8 @@ __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const in
   float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int i = group; i < n; i += kGroups) {
-    const float2 w = ml[(int64_t)i * a.part_rows];
-    const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)i * a.part_rows * D + ch);
+    const float2 w = a.part_ml[piece(i)];
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + piece(i) * D + ch);
     const float f = __builtin_amdgcn_exp2f(w.x - ref);
     l += f * w.y;
     x[0] += f * y.x;
@@ -423,9 +433,10 @@ void by_type(int d, int dtype, bool e4m3, F&& f) {
 }  // namespace
 
 void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_rows, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)a.tiles * a.c.hkv * a.splits));
+  const dim3 grid((unsigned)(a.workers ? a.workers : (int64_t)a.tiles * a.c.hkv * a.splits));
   by_type(d, dtype, e4m3, [&](auto t, auto dd, auto f8) {
-    if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
+    if (tile_rows == 32 && a.part_rows <= 16) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 16><<<grid, dim3(256), 0, st>>>(a);
+    else if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 32><<<grid, dim3(256), 0, st>>>(a);
     else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
   });
 }
@@ -433,7 +444,7 @@ void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_ro
 void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m3, hipStream_t st) {
   const int64_t rows = (int64_t)a.c.n_tokens * a.c.hq;
   by_type(d, dtype, false, [&](auto t, auto dd, auto) {
-    if (a.splits > 8) merge_kernel<decltype(t), decltype(dd)::value, 4><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a, tile_rows, e4m3);
+    if (a.workers ? rows * 8 < a.workers : a.splits > 8) merge_kernel<decltype(t), decltype(dd)::value, 4><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a, tile_rows, e4m3);
     else merge_kernel<decltype(t), decltype(dd)::value, 1><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st>>>(a, tile_rows, e4m3);
   });
 }

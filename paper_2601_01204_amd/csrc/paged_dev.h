@@ -59,6 +59,8 @@ struct AttendArgs {
   int32_t splits;               // key ranges per row tile
   int32_t split_keys;           // keys of a range, a multiple of 64
   int32_t part_rows;            // rows a block has in part_o
+  int32_t workers;              // launches of few rows: workgroups that share the keys of all columns evenly, two places each in part_o;
+                                // 0: a workgroup to each column
 };
 
 struct EvictArgs {

@@ -147,6 +147,152 @@ struct RowBlock {
   }
 };
 
+// Up to ROWS (16 or 32) query rows of one wave, in launches of few rows: the same products from 16 x 16 x 32 instructions where 16 rows are
+// enough, which halves the registers of queries and outputs.  A row has 64 / ROWS lanes; lane part `j` of them holds the logits of
+// keys kSpan (r / 4) + 4 j + r % 4, and of the output the channels kSpan q + 4 j .. + 3, quad by quad.
+template <typename T, int D, bool E4M3, int ROWS>
+struct FewRows {
+  typedef Shape<D, E4M3> S;
+  static constexpr int kSpan = 256 / ROWS;             // 16 or 8
+  static constexpr int kLogits = ROWS / 2;             // of a lane, for 32 keys
+  static constexpr int kSteps = D * ROWS / 512;        // matrix instructions of 16 or 32 channels
+  static constexpr int kQuads = D / kSpan;
+  typedef float acc_t __attribute__((ext_vector_type(ROWS == 32 ? 16 : 4)));
+  static constexpr int kBlocks = D / ROWS;             // accumulators of ROWS channels
+  u32x4 q[kSteps];
+  acc_t o[kBlocks];
+  float m, l;                                          // in log2 units; l: this lane's part of the keys
+  int lo, hi;                                          // keys [lo, hi) are seen by this lane's row
+
+  static __device__ __forceinline__ acc_t mfma(u32x4 a, u32x4 b, acc_t c) {
+    if constexpr (ROWS == 32) return T::mfma(a, b, c);
+    else return T::mfma16(a, b, c);
+  }
+  // First channel of the octet that lane part j brings to step s of the first product.
+  static __device__ __forceinline__ int channel(int s, int j) {
+    constexpr int kPart = 64 / ROWS;
+    return E4M3 ? 16 * kPart * (s >> 1) + 16 * j + 8 * (s & 1) : 8 * kPart * s + 8 * j;
+  }
+  __device__ __forceinline__ float quad(int i, int e) const { return o[ROWS == 32 ? i >> 2 : i][ROWS == 32 ? 4 * (i & 3) + e : e]; }
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) o[b] = acc_t{};
+    m = -kInf;
+    l = 0.f;
+  }
+  __device__ __forceinline__ void load_queries(const uint8_t* row, int j) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = *reinterpret_cast<const u32x4*>(row + 2 * channel(s, j));
+  }
+  // A value per lane part joined over a row's lanes.
+  template <typename F>
+  static __device__ __forceinline__ float over_row(float x, F&& f) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    if constexpr (ROWS == 16) {
+      const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      x = f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
+    return x;
+  }
+
+  // Logits of the 32 keys whose rows begin at `k` in LDS.
+  __device__ __forceinline__ void logits(const uint8_t* k, int lane, float (&x)[kLogits]) const {
+    const int row = lane % ROWS, j = lane / ROWS;
+#pragma unroll
+    for (int part = 0; part < 32 / ROWS; ++part) {
+      acc_t s{};
+      const int at = row + part * ROWS;
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int i = 0; i < kSteps / 2; ++i) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(k + lds_offset<S::kRowBytes>(at, channel(2 * i, j) / 16));
+          s = mfma(widen<T>((u32x2){w[0], w[1]}), q[2 * i], s);
+          s = mfma(widen<T>((u32x2){w[2], w[3]}), q[2 * i + 1], s);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) s = mfma(*reinterpret_cast<const u32x4*>(k + lds_offset<S::kRowBytes>(at, channel(i, j) / 8)), q[i], s);
+      }
+#pragma unroll
+      for (int r = 0; r < (ROWS == 32 ? 16 : 4); ++r) x[4 * part + r] = s[r];
+    }
+  }
+
+  // V^T fragment: ROWS channels from ROWS * b on, the keys of logits 8 t .. 8 t + 7 of every lane part.
+  static __device__ __forceinline__ u32x4 value_fragment(const uint8_t* v, int lane, int t, int b) {
+    const int j = lane / ROWS, i = lane & 15, c0 = ROWS * b + (ROWS == 32 ? 16 * ((lane >> 4) & 1) : 0);
+    const int first = 2 * kSpan * t + 4 * j;           // key of the first four logits, the other four kSpan further
+    if constexpr (E4M3) {
+      const int row = first + ((i >> 1) & 3) + kSpan * (i >> 3);
+      const uint8_t* p = v + lds_offset<S::kRowBytes>(row, c0 / 16) + 8 * (i & 1);
+      return widen<T>(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)p)));
+    } else {
+      const int row = first + (i >> 2), chunk = c0 / 8 + ((i & 3) >> 1);
+      const uint8_t* p0 = v + lds_offset<S::kRowBytes>(row, chunk) + 8 * (i & 1);
+      const uint8_t* p1 = v + lds_offset<S::kRowBytes>(row + kSpan, chunk) + 8 * (i & 1);
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p0));
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p1));
+      return (u32x4){x[0], x[1], y[0], y[1]};
+    }
+  }
+
+  // What the row of this lane does not see becomes -infinity.  key0: first of the 32 keys; absent: keys without a page.
+  __device__ __forceinline__ void mask(float (&x)[kLogits], int key0, uint32_t absent, int j) const {
+    const int first = key0 + 4 * j;
+    absent >>= 4 * j;
+#pragma unroll
+    for (int r = 0; r < kLogits; ++r) {
+      const int off = kSpan * (r >> 2) + (r & 3), key = first + off;
+      x[r] = (key < hi && key >= lo && !((absent >> off) & 1)) ? x[r] : -kInf;
+    }
+  }
+
+  // The probabilities in place of the logits (c: softmax scale * log2 e), and their sum; raises m where it has to.
+  __device__ __forceinline__ void soften(float (&x)[kLogits], float c) {
+    float top = fmaxf(x[0], x[1]);
+#pragma unroll
+    for (int r = 2; r < kLogits; ++r) top = fmaxf(top, x[r]);
+    top = c * over_row(top, [](float a, float b) { return fmaxf(a, b); });
+    if (__ballot(top > m + kGap)) {                      // (also the first key of a row, whose m is -infinity)
+      const float next = fmaxf(m, top), alpha = next == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - next);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < (ROWS == 32 ? 16 : 4); ++r) o[b][r] *= alpha;
+      l *= alpha;
+      m = next;
+    }
+    const float ref = m == -kInf ? 0.f : m;
+#pragma unroll
+    for (int r = 0; r < kLogits; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], c, -ref));
+      l += x[r];
+    }
+  }
+
+  // O += P V, with probabilities as a pair of 16-bit values, so that they are not rounded before the output is (the matrix cores have time).
+  __device__ __forceinline__ void add_values(const float (&x)[kLogits], const uint8_t* v, int lane) {
+#pragma unroll
+    for (int t = 0; t < kLogits / 8; ++t) {
+      u32x4 p, p_low;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = x[8 * t + 2 * e], x1 = x[8 * t + 2 * e + 1];
+        p[e] = T::pack(x0, x1);
+        p_low[e] = T::pack(x0 - T::low(p[e]), x1 - T::high(p[e]));
+      }
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const u32x4 f = value_fragment(v, lane, t, b);
+        o[b] = mfma(f, p, o[b]);
+        o[b] = mfma(f, p_low, o[b]);
+      }
+    }
+  }
+};
+
 // The page of key `key` of a sequence of `len` tokens (one lane a key): keys behind the end take the last one's.
 __device__ __forceinline__ int32_t page_of_key(const Call& c, int b, int key, int len) {
   return page_of(c, b, min(key, len - 1) >> c.page_shift);
@@ -218,6 +364,58 @@ __device__ __forceinline__ int splits_of(const AttendArgs& a, const Range& r) {
 }
 __device__ __forceinline__ int split_end(const AttendArgs& a, const Range& r, int split) {
   return split == a.splits - 1 ? r.hi : min(r.hi, r.lo + (split + 1) * a.split_keys);
+}
+
+// ---- launches of few rows: a column is a sequence's keys for one key head, a unit kFewKeys of them ----------------------
+constexpr int kFewKeys = 128;
+__device__ __forceinline__ int units_of(const AttendArgs& a, int b) {
+  const Seq s = sequence(a.c, b);
+  if (s.n == 0) return 0;
+  const Range r = tile_range(a, s, 0, s.n * a.c.group);
+  return r.hi > r.lo ? (r.hi - r.lo + kFewKeys - 1) / kFewKeys : 0;
+}
+// Units of the sequences in front of sequence b, of one key head (all lanes of a wave together).
+__device__ __forceinline__ int units_before(const AttendArgs& a, int b) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int base = 0; base < b; base += 64) sum += base + lane < b ? units_of(a, base + lane) : 0;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  return sum;
+}
+// Units of a worker's share: columns one after the other (sequence by sequence, head by head) are cut into even shares.
+__device__ __forceinline__ int share_of(const AttendArgs& a, int total) { return max(1, (total + a.workers - 1) / a.workers); }
+
+struct Column {
+  int b, head;
+  int first, units;             // among all units
+};
+// The column of unit `unit`, which is one.
+__device__ __forceinline__ Column column_of(const AttendArgs& a, int unit) {
+  const int lane = threadIdx.x & 63, hkv = a.c.hkv;
+  int before = 0;               // units of one head of the sequences passed
+  for (int base = 0; base < a.c.n_seqs; base += 64) {
+    const int mine = base + lane < a.c.n_seqs ? units_of(a, base + lane) : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const int all = __shfl(upto, 63);
+    if (unit < (before + all) * hkv) {
+      const int at = __popcll(__ballot((before + upto) * hkv <= unit));
+      const int first = before + __shfl(upto, at) - __shfl(mine, at), units = __shfl(mine, at);
+      Column c;
+      c.b = base + at;
+      c.head = (unit - first * hkv) / units;
+      c.first = first * hkv + c.head * units;
+      c.units = units;
+      return c;
+    }
+    before += all;
+  }
+  return Column{0, 0, 0, 0};    // (not reached)
 }
 
 }  // namespace paged
