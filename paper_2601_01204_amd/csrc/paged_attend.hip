@@ -47,23 +47,30 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
   const int ld_row = lane / kLPR * kLoads, ld_chunk = lane % kLPR;
 
   int unit = 0, unit_end = 1;                                // this workgroup's units; without workers: one column, whatever it holds
+  Lanes lanes;
   if (a.workers) {
-    const int total = units_before(a, c.n_seqs) * c.hkv, share = share_of(a, total);
+    lanes = load_lanes(a, 0, 0);
+    int total = lanes.all;
+    for (int base = 64; base < c.n_seqs; base += 64) total += load_lanes(a, base, 0).all;
+    total *= c.hkv;
+    const int share = share_of(a, total);
     unit = blockIdx.x * share;
     unit_end = min(total, unit + share);
   }
   while (unit < unit_end) {
     Column col;
     if (a.workers) {
-      col = column_of(a, unit);
+      col = column_of(a, unit, lanes);
     } else {
       col.b = blockIdx.x / c.hkv;
       col.head = blockIdx.x - col.b * c.hkv;
+      col.s = sequence(c, col.b);
       col.first = 0;
       col.units = 1;
     }
-    const int b = col.b, head = col.head;
-    const Seq s = sequence(c, b);
+    // (the same in all lanes: in scalar registers)
+    const int b = __builtin_amdgcn_readfirstlane(col.b), head = __builtin_amdgcn_readfirstlane(col.head);
+    const Seq s{__builtin_amdgcn_readfirstlane(col.s.first), __builtin_amdgcn_readfirstlane(col.s.n), __builtin_amdgcn_readfirstlane(col.s.len)};
     const int n_rows = s.n * c.group;
     if (n_rows == 0) return;                                 // (a column of a worker has rows)
     const Range range = tile_range(a, s, 0, n_rows);
@@ -344,22 +351,35 @@ __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const in
   const int64_t job = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   const int token = (int)(job / c.hq), qh = (int)(job - (int64_t)token * c.hq);
   if (token >= c.n_tokens) return;
-  const int b = sequence_of_row(c, token);
-  if (b < 0) return;
-  const Seq s = sequence(c, b);
-  const int i_row = token - s.first;
-  if (i_row < 0 || i_row >= s.n) return;
-  const int head = qh / c.group, row = i_row * c.group + qh - head * c.group;
+  const int head = qh / c.group;
   int64_t first;                                             // the first piece's place among the pieces of part_rows rows each
-  int n, apart = 1;                                          // and from one to the next
+  int n, apart = 1, row;                                     // how many, and from one to the next; the row within its sequence
   if (a.workers) {
     // a worker's places: 0 for a column that began before it, 1 for one that ends behind it, so the first piece lies in a 1, others in a 0
-    const int units = units_of(a, b), before = units_before(a, b) * c.hkv + head * units, share = share_of(a, units_before(a, c.n_seqs) * c.hkv);
-    const int w0 = before / share;
-    n = units ? (before + units - 1) / share - w0 + 1 : 0;
+    int before = 0, units = -1, in_front = 0;
+    for (int base = 0; base < c.n_seqs; base += 64) {
+      const Lanes x = load_lanes(a, base, before);
+      const uint64_t mine = __ballot(token >= x.mine.first && token < x.mine.first + x.mine.n);
+      if (units < 0 && mine) {
+        const int at = __ffsll((unsigned long long)mine) - 1;
+        units = __shfl(x.units, at);
+        in_front = before + __shfl(x.upto, at) - units;
+        row = (token - __shfl(x.mine.first, at)) * c.group + qh - head * c.group;
+      }
+      before += x.all;
+    }
+    if (units < 0) return;
+    const int begin = in_front * c.hkv + head * units, share = share_of(a, before * c.hkv), w0 = begin / share;
+    n = units ? (begin + units - 1) / share - w0 + 1 : 0;
     first = (int64_t)w0 * 2;
     apart = 2;
   } else {
+    const int b = sequence_of_row(c, token);
+    if (b < 0) return;
+    const Seq s = sequence(c, b);
+    const int i_row = token - s.first;
+    if (i_row < 0 || i_row >= s.n) return;
+    row = i_row * c.group + qh - head * c.group;
     const int t = row / tile_rows, row0 = t * tile_rows;
     n = splits_of(a, tile_range(a, s, row0, min(tile_rows, s.n * c.group - row0)));
     first = ((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits;

@@ -368,54 +368,56 @@ __device__ __forceinline__ int split_end(const AttendArgs& a, const Range& r, in
 
 // ---- launches of few rows: a column is a sequence's keys for one key head, a unit kFewKeys of them ----------------------
 constexpr int kFewKeys = 128;
-__device__ __forceinline__ int units_of(const AttendArgs& a, int b) {
-  const Seq s = sequence(a.c, b);
+__device__ __forceinline__ int units_of(const AttendArgs& a, const Seq& s) {
   if (s.n == 0) return 0;
   const Range r = tile_range(a, s, 0, s.n * a.c.group);
   return r.hi > r.lo ? (r.hi - r.lo + kFewKeys - 1) / kFewKeys : 0;
 }
-// Units of the sequences in front of sequence b, of one key head (all lanes of a wave together).
-__device__ __forceinline__ int units_before(const AttendArgs& a, int b) {
-  const int lane = threadIdx.x & 63;
-  int sum = 0;
-  for (int base = 0; base < b; base += 64) sum += base + lane < b ? units_of(a, base + lane) : 0;
+// Sixty-four sequences, one a lane, with the units of one key head in front of and in them.
+struct Lanes {
+  int base;                     // sequence of lane 0
+  Seq mine;
+  int units, upto;              // of this lane's sequence; up to it within the sixty-four
+  int before, all;              // in front of the sixty-four; in all of them
+};
+__device__ __forceinline__ Lanes load_lanes(const AttendArgs& a, int base, int before) {
+  const int lane = threadIdx.x & 63, b = base + lane;
+  Lanes x;
+  x.base = base;
+  x.before = before;
+  x.mine = Seq{0, 0, 0};
+  if (b < a.c.n_seqs) x.mine = sequence(a.c, b);
+  x.units = units_of(a, x.mine);
+  x.upto = x.units;
 #pragma unroll
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  return sum;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x.upto, o);
+    if (lane >= o) x.upto += y;
+  }
+  x.all = __shfl(x.upto, 63);
+  return x;
 }
 // Units of a worker's share: columns one after the other (sequence by sequence, head by head) are cut into even shares.
 __device__ __forceinline__ int share_of(const AttendArgs& a, int total) { return max(1, (total + a.workers - 1) / a.workers); }
 
 struct Column {
   int b, head;
+  Seq s;
   int first, units;             // among all units
 };
-// The column of unit `unit`, which is one.
-__device__ __forceinline__ Column column_of(const AttendArgs& a, int unit) {
-  const int lane = threadIdx.x & 63, hkv = a.c.hkv;
-  int before = 0;               // units of one head of the sequences passed
-  for (int base = 0; base < a.c.n_seqs; base += 64) {
-    const int mine = base + lane < a.c.n_seqs ? units_of(a, base + lane) : 0;
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
-    const int all = __shfl(upto, 63);
-    if (unit < (before + all) * hkv) {
-      const int at = __popcll(__ballot((before + upto) * hkv <= unit));
-      const int first = before + __shfl(upto, at) - __shfl(mine, at), units = __shfl(mine, at);
-      Column c;
-      c.b = base + at;
-      c.head = (unit - first * hkv) / units;
-      c.first = first * hkv + c.head * units;
-      c.units = units;
-      return c;
-    }
-    before += all;
-  }
-  return Column{0, 0, 0, 0};    // (not reached)
+// The column of unit `unit`, which is one and no earlier than `x`'s sequences; x moves on to its sequences.
+__device__ __forceinline__ Column column_of(const AttendArgs& a, int unit, Lanes& x) {
+  const int hkv = a.c.hkv;
+  while (unit >= (x.before + x.all) * hkv) x = load_lanes(a, x.base + 64, x.before + x.all);
+  const int at = __popcll(__ballot((x.before + x.upto) * hkv <= unit));
+  Column c;
+  c.units = __shfl(x.units, at);
+  const int first = x.before + __shfl(x.upto, at) - c.units;
+  c.b = x.base + at;
+  c.s = Seq{__shfl(x.mine.first, at), __shfl(x.mine.n, at), __shfl(x.mine.len, at)};
+  c.head = (unit - first * hkv) / c.units;
+  c.first = first * hkv + c.head * c.units;
+  return c;
 }
 
 }  // namespace paged

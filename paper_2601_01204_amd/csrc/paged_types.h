@@ -73,7 +73,7 @@ __device__ __forceinline__ Seq sequence(const Call& c, int b) {
   s.first = min(max(a0, 0), c.n_tokens);
   s.n = min(max(min(a1, c.n_tokens) - s.first, 0), c.max_new);
   s.len = min(max(l0, 0), c.max_len);
-  if ((s.first != a0 || s.first + s.n != a1 || s.len != l0) && (threadIdx.x & 63) == 0) atomicOr(c.status, kStatusLength);
+  if (s.first != a0 || s.first + s.n != a1 || s.len != l0) atomicOr(c.status, kStatusLength);
   return s;
 }
 // Page number of entry `entry` of sequence b; -1 for one outside the pool.
