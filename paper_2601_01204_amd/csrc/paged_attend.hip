@@ -54,8 +54,8 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     for (int base = 64; base < c.n_seqs; base += 64) total += load_lanes(a, base, 0).all;
     total *= c.hkv;
     const int share = share_of(a, total);
-    unit = blockIdx.x * share;
-    unit_end = min(total, unit + share);
+    unit = uniform(blockIdx.x * share);
+    unit_end = uniform(min(total, unit + share));
   }
   while (unit < unit_end) {
     Column col;
@@ -68,16 +68,15 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
       col.first = 0;
       col.units = 1;
     }
-    // (the same in all lanes: in scalar registers)
-    const int b = __builtin_amdgcn_readfirstlane(col.b), head = __builtin_amdgcn_readfirstlane(col.head);
-    const Seq s{__builtin_amdgcn_readfirstlane(col.s.first), __builtin_amdgcn_readfirstlane(col.s.n), __builtin_amdgcn_readfirstlane(col.s.len)};
+    const int b = uniform(col.b), head = uniform(col.head);
+    const Seq s = uniform(col.s);
     const int n_rows = s.n * c.group;
     if (n_rows == 0) return;                                 // (a column of a worker has rows)
     const Range range = tile_range(a, s, 0, n_rows);
-    const int upto = min(unit_end, col.first + col.units);
+    const int upto = uniform(min(unit_end, col.first + col.units));
     const bool whole = unit == col.first && upto == col.first + col.units;
-    const int k0 = a.workers ? range.lo + (unit - col.first) * kFewKeys : range.lo;
-    const int k1 = a.workers ? min(range.hi, range.lo + (upto - col.first) * kFewKeys) : range.hi;
+    const int k0 = uniform(a.workers ? range.lo + (unit - col.first) * kFewKeys : range.lo);
+    const int k1 = uniform(a.workers ? min(range.hi, range.lo + (upto - col.first) * kFewKeys) : range.hi);
 
     W w;
     w.clear();
@@ -201,6 +200,10 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 }
 
 // ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
+// Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is d / 4 matrix cycles x 16 (512 for d = 128) and some 290
+// vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
+// before it goes through its exponentials, then the second product of that one.  K is staged two tiles ahead and V one, three tiles of K
+// and two of V in LDS, one barrier a tile; loads are issued half a tile before they are stored.
 constexpr int kChunkRows = 128;
 
 template <typename T, int D, bool E4M3>
@@ -208,7 +211,8 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   typedef Shape<D, E4M3> S;
   constexpr int kRB = S::kRowBytes, kLPR = S::kLanesPerRow;
   constexpr int kLoads = 64 * kLPR / 256;
-  __shared__ __align__(16) uint8_t lds[2][2][64 * kRB];      // [buffer][K, V]
+  constexpr int kTile = 64 * kRB;
+  __shared__ __align__(16) uint8_t lds[5 * kTile];           // K, K, K, V, V
 
   const Call& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
@@ -217,14 +221,16 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   const int head = column % c.hkv, split = column / c.hkv;
   int b, t;
   if (!find_tile(a, tile, kChunkRows, b, t)) return;
-  const Seq s = sequence(c, b);
+  b = uniform(b);
+  t = uniform(t);
+  const Seq s = uniform(sequence(c, b));
   const int rows = s.n * c.group, row0 = t * kChunkRows;
   if (row0 >= rows) return;
   const int n_rows = min(kChunkRows, rows - row0);
   const Range range = tile_range(a, s, row0, n_rows);
   const int n_splits = splits_of(a, range);
   if (split >= n_splits) return;
-  const int k0 = range.lo + split * a.split_keys, k1 = split_end(a, range, split);
+  const int k0 = uniform(range.lo + split * a.split_keys), k1 = uniform(split_end(a, range, split));
 
   RowBlock<T, D, E4M3> w;
   w.clear();
@@ -236,87 +242,111 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   w.lo = a.window > 0 ? place + 1 - a.window : 0;
   w.load_queries(a.q.p + (int64_t)(s.first + i_row) * a.q.tok + (int64_t)(head * c.group + g_row) * a.q.head, h);
   const int place_first = s.len - s.n + first / c.group, place_last = s.len - s.n + last / c.group;
-  const int all_hi = a.causal ? min(s.len, place_first + 1) : s.len, any_hi = first > last ? 0 : (a.causal ? min(s.len, place_last + 1) : s.len);
-  const int all_lo = a.window > 0 ? place_last + 1 - a.window : 0, any_lo = a.window > 0 ? place_first + 1 - a.window : 0;
+  // keys [all_lo, all_hi) are seen by every row of the wave, keys outside [any_lo, any_hi) by none
+  const int all_hi = uniform(a.causal ? min(s.len, place_first + 1) : s.len), any_hi = uniform(first > last ? 0 : (a.causal ? min(s.len, place_last + 1) : s.len));
+  const int all_lo = uniform(a.window > 0 ? place_last + 1 - a.window : 0), any_lo = uniform(a.window > 0 ? place_first + 1 - a.window : 0);
   const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
 
   const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR;
   const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
   const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
-  u32x4 rk[kLoads], rv[kLoads];
-  uint64_t absent_loaded = 0;                                // of the tile in the registers
-  int32_t page = 0;
+  u32x4 r[kLoads];                                           // rows on their way: of K and of V in turn
+  int32_t page = 0;                                          // of a tile's keys, one a lane: the tile whose rows are loaded next
+  uint64_t absent_loaded = 0;                                // keys without a page: of the tile of V in the registers
   auto fetch_page = [&](int u) { page = u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
-  auto fetch_rows = [&](int u) {
-    absent_loaded = __ballot(page < 0);
-    if (absent_loaded && threadIdx.x == 0) note_bad_page(c);
+  auto fetch = [&](const uint8_t* p, int u) {
     const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      rk[i] = *reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride);
-      rv[i] = *reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride);
-    }
+    for (int i = 0; i < kLoads; ++i) r[i] = *reinterpret_cast<const u32x4*>(p + at + i * c.slot_stride);
   };
-  auto put_rows = [&](int buf, int u) {
-    const bool tail = u + 64 > s.len || absent_loaded;
+  auto fetch_v = [&](int u) {
+    absent_loaded = __ballot(page < 0);
+    if (absent_loaded && threadIdx.x == 0) note_bad_page(c);
+    fetch(vp, u);
+  };
+  auto put = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = ld_row + i;
-      if (tail && (u + r >= s.len || ((absent_loaded >> r) & 1))) rv[i] = (u32x4){0, 0, 0, 0};
-      *reinterpret_cast<u32x4*>(lds[buf][0] + lds_offset<kRB>(r, ld_chunk)) = rk[i];
-      *reinterpret_cast<u32x4*>(lds[buf][1] + lds_offset<kRB>(r, ld_chunk)) = rv[i];
-    }
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lds + buf * kTile + lds_offset<kRB>(ld_row + i, ld_chunk)) = r[i];
   };
+  auto put_v = [&](int buf, int u) {                         // values behind the end and without a page are zero
+    if (u + 64 > s.len || absent_loaded)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if (u + ld_row + i >= s.len || ((absent_loaded >> (ld_row + i)) & 1)) r[i] = (u32x4){0, 0, 0, 0};
+    put(3 + buf);
+  };
+  auto live = [&](int key0) { return key0 < k1 && key0 < any_hi && key0 + 32 > any_lo; };
 
-  uint64_t absent = 0;
+  // in LDS before the first tile: its K and V and the next one's K; on the way: the next one's V
+  uint64_t absent = 0;                                       // of the running tile
+  f32x16 x, y;                                               // logits of the running unit, then its probabilities; of the next one
   if (k0 < k1) {
     fetch_page(k0);
-    fetch_rows(k0);
-    fetch_page(k0 + 64);
-    put_rows(0, k0);
+    fetch(kp, k0);
+    put(0);
+    fetch_v(k0);
+    put_v(0, k0);
     absent = absent_loaded;
+    fetch_page(k0 + 64);
     if (k0 + 64 < k1) {
-      fetch_rows(k0 + 64);
+      fetch(kp, k0 + 64);
+      put(1);
+      fetch_v(k0 + 64);
       fetch_page(k0 + 128);
     }
   }
   __syncthreads();
-  int buf = 0;
-  for (int u = k0; u < k1; u += 64, buf ^= 1) {
+  int kb = 0, vb = 0;                                        // buffers of the running tile
+  if (live(k0)) x = w.logits(lds, lane);
+  for (int u = k0; u < k1; u += 64) {
+    const int kb1 = kb == 2 ? 0 : kb + 1, kb2 = kb1 == 2 ? 0 : kb1 + 1;
+    uint64_t absent_next = 0;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int key0 = u + 32 * half;
-      if (key0 < any_hi && key0 + 32 > any_lo) {
-        f32x16 x = w.logits(lds[buf][0] + half * 32 * kRB, lane);
+      const uint8_t* const k_now = lds + kb * kTile + half * 32 * kRB;
+      const uint8_t* const k_next = half == 0 ? lds + kb * kTile + 32 * kRB : lds + kb1 * kTile;
+      const uint8_t* const v_now = lds + (3 + vb) * kTile + half * 32 * kRB;
+      const bool now = live(key0), next = live(key0 + 32);
+      if (now) {
         const uint32_t missing = (uint32_t)(absent >> (32 * half));
-        if (key0 + 32 > all_hi || key0 < all_lo || missing) w.mask(x, key0, missing, h);
-        w.soften(x, factor);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) w.l += x[r];
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          u32x4 p;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = T::pack(x[8 * st + 2 * e], x[8 * st + 2 * e + 1]);
-#pragma unroll
-          for (int cb = 0; cb < S::kBlocks; ++cb) w.o[cb] = T::mfma(w.value_fragment(lds[buf][1] + half * 32 * kRB, lane, st, cb), p, w.o[cb]);
+        const bool masked = key0 + 32 > all_hi || key0 < all_lo || missing;
+        if (masked) w.mask(x, key0, missing, h);
+        float sum = next ? w.template soften<true>(x, factor, k_next, lane, y) : w.template soften<false>(x, factor, k_next, lane, y);
+        if (__ballot(sum > kMost || w.m == -kInf)) {         // rare: form the unit again and raise m to its largest
+          x = w.logits(k_now, lane);
+          if (masked) w.mask(x, key0, missing, h);
+          w.raise(x, factor);
+          sum = w.template soften<false>(x, factor, k_next, lane, y);
         }
+        w.l += sum;
+        w.add_values(x, v_now, lane);
+      } else if (next) {
+        y = w.logits(k_next, lane);
       }
-    }
-    if (u + 64 < k1) {
-      put_rows(buf ^ 1, u + 64);                             // read last in the tile before this one, a barrier ago
-      absent = absent_loaded;
-      if (u + 128 < k1) {
-        fetch_rows(u + 128);
+      x = y;
+      // into buffers that were read last in the tile before this one, a barrier ago
+      if (half == 0) {
+        if (u + 64 < k1) {
+          put_v(vb ^ 1, u + 64);
+          absent_next = absent_loaded;
+        }
+        if (u + 128 < k1) fetch(kp, u + 128);
+      } else if (u + 128 < k1) {
+        put(kb2);
+        fetch_v(u + 128);
         fetch_page(u + 192);
       }
     }
     __syncthreads();
+    kb = kb1;
+    vb ^= 1;
+    absent = absent_next;
   }
 
   {
-    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
-    w.l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
+    w.l = __uint_as_float(z[0]) + __uint_as_float(z[1]);
   }
   if (first + (lane & 31) > last) return;
   const int token = s.first + i_row, qh = head * c.group + g_row;

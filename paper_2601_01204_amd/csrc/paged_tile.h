@@ -13,8 +13,10 @@
 // final division.  A row of 8-bit keys is read 16 channels at a time, which serve two matrix instructions: their
 // channels are 32 s + 16 h + 0..7 and 8..15, for the queries too.
 //
-// Softmax.  p = 2^(c s - m) in fp32 with m the largest c s of the row so far, raised only where a key lies more than kGap above it
-// (p stays below 2^kGap, and O and l are rescaled in a rare, wave-uniform branch).  Row sums are taken before
+// Softmax.  p = 2^(c s - m) in fp32.  Few rows: m is the largest c s of the row so far, raised only where a key lies more than kGap above
+// it (p stays below 2^kGap, and O and l are rescaled in a rare, wave-uniform branch).  More rows, where vector instructions are dear: m is
+// the largest of the row's first unit, and no maximum is taken after that; only where a unit's sum shows that some p is large (kMost,
+// which fp16 still holds) is the unit formed again and m raised.  Row sums are taken before
 // the probabilities are rounded for the second product, so that the lse is as exact as the logits.
 #pragma once
 #include "paged_types.h"
@@ -25,6 +27,7 @@ namespace kvx {
 namespace paged {
 
 constexpr float kGap = 8.0f;
+constexpr float kMost = 32768.0f;
 constexpr float kInf = __builtin_inff();
 
 template <int ROW_BYTES>
@@ -123,8 +126,8 @@ struct RowBlock {
     }
   }
 
-  // The unit's probabilities, in place of its logits (c: softmax scale * log2 e); raises m where it has to.
-  __device__ __forceinline__ void soften(f32x16& s, float c) {
+  // m rises to the largest of the unit's logits.
+  __device__ __forceinline__ void raise(const f32x16& s, float c) {
     float top = fmaxf(s[0], s[1]);
 #pragma unroll
     for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
@@ -132,18 +135,72 @@ struct RowBlock {
       const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = c * fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
     }
-    if (__ballot(top > m + kGap)) {                      // (also the first key of a row, whose m is -infinity)
-      const float next = fmaxf(m, top), alpha = next == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - next);
+    const float next = fmaxf(m, top), alpha = next == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - next);
 #pragma unroll
-      for (int b = 0; b < S::kBlocks; ++b)
+    for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[b][r] *= alpha;
-      l *= alpha;
-      m = next;
-    }
+      for (int r = 0; r < 16; ++r) o[b][r] *= alpha;
+    l *= alpha;
+    m = next;
+  }
+  // Fragment i of the unit's keys as it lies in LDS: a step's, or for 8-bit keys those of steps 2 i and 2 i + 1.
+  static __device__ __forceinline__ u32x4 key_fragment(const uint8_t* k, int lane, int i) {
+    return *reinterpret_cast<const u32x4*>(k + lds_offset<S::kRowBytes>(lane & 31, 2 * i + (lane >> 5)));
+  }
+  // The unit's probabilities in place of its logits `s` (c: softmax scale * log2 e, m as it is), and their sum; with NEXT, the logits `y` of the
+  // unit whose keys begin at `k`.  A matrix instruction (32 cycles) depends on the one before it and a wave issues in order, so the vector
+  // instructions are put between them: 16 / kSteps logits behind each.
+  template <bool NEXT>
+  __device__ __forceinline__ float soften(f32x16& s, float c, const uint8_t* k, int lane, f32x16& y) const {
+    constexpr int kPer = 16 / S::kSteps;
     const float ref = m == -kInf ? 0.f : m;
+    u32x4 kf[2];
+    if constexpr (NEXT) {
+      kf[0] = key_fragment(k, lane, 0);
+      kf[1] = key_fragment(k, lane, 1);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref));
+      for (int r = 0; r < 16; ++r) y[r] = 0.f;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < S::kSteps; ++i) {
+      if constexpr (NEXT) {
+        if constexpr (E4M3) {
+          const u32x4 f = kf[(i >> 1) & 1];
+          y = T::mfma(widen<T>((u32x2){f[2 * (i & 1)], f[2 * (i & 1) + 1]}), q[i], y);
+          if ((i & 1) && i + 3 < S::kSteps) kf[(i >> 1) & 1] = key_fragment(k, lane, (i >> 1) + 2);
+        } else {
+          y = T::mfma(kf[i & 1], q[i], y);
+          if (i + 2 < S::kSteps) kf[i & 1] = key_fragment(k, lane, i + 2);
+        }
+      }
+#pragma unroll
+      for (int r = i * kPer; r < (i + 1) * kPer; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref));
+        sum += s[r];
+      }
+      if constexpr (NEXT) __builtin_amdgcn_sched_barrier(0);
+    }
+    return sum;
+  }
+
+  // O += P V, the probabilities rounded to 16 bits.
+  __device__ __forceinline__ void add_values(const f32x16& x, const uint8_t* v, int lane) {
+    constexpr int kAll = 2 * S::kBlocks;
+    u32x4 vf[2] = {value_fragment(v, lane, 0, 0), value_fragment(v, lane, 1 / S::kBlocks, 1 % S::kBlocks)}, p[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[0][e] = T::pack(x[2 * e], x[2 * e + 1]);
+#pragma unroll
+    for (int n = 0; n < kAll; ++n) {
+      const int t = n / S::kBlocks, b = n % S::kBlocks;
+      o[b] = T::mfma(vf[n & 1], p[t], o[b]);
+      if (n + 2 < kAll) vf[n & 1] = value_fragment(v, lane, (n + 2) / S::kBlocks, (n + 2) % S::kBlocks);
+      if (n < S::kBlocks) {
+#pragma unroll
+        for (int e = n * 4 / S::kBlocks; e < (n + 1) * 4 / S::kBlocks; ++e) p[1][e] = T::pack(x[8 + 2 * e], x[9 + 2 * e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 };
 

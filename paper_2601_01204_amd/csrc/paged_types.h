@@ -76,6 +76,9 @@ __device__ __forceinline__ Seq sequence(const Call& c, int b) {
   if (s.first != a0 || s.first + s.n != a1 || s.len != l0) atomicOr(c.status, kStatusLength);
   return s;
 }
+// What is the same in all lanes, in scalar registers: branches on it are scalar too.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Seq uniform(const Seq& s) { return Seq{uniform(s.first), uniform(s.n), uniform(s.len)}; }
 // Page number of entry `entry` of sequence b; -1 for one outside the pool.
 __device__ __forceinline__ int32_t page_of(const Call& c, int b, int entry) {
   const int32_t page = c.table[(int64_t)b * c.table_stride + entry];
