@@ -7,6 +7,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <cstdlib>
 #include <new>
 #include <string>
 #include <vector>
@@ -55,7 +56,7 @@ int fail(kv_paged* h, int code, const char* fmt, ...) {
 
 int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kFewRows = 32, kChunkRows = 128;      // row tiles of the two attention kernels
+constexpr int kFewRows = 32, kChunkRows = 128, kLargeRows = 256;      // row tiles of the attention kernels
 
 int check_config(const kv_paged_config* c) {
   if (!c) return fail(nullptr, KV_E_INVAL, "kv_paged_init: cfg is NULL");
@@ -153,9 +154,9 @@ int check_call(kv_paged* h, const char* call, const kv_pages* p, const kv_paged_
   if (!b->q_start || !b->kv_lens) return fail(h, KV_E_INVAL, "%s: q_start or kv_lens is NULL", call);
   if (!p->k || !p->v || !p->page_table) return fail(h, KV_E_INVAL, "%s: pages: NULL pointer", call);
   if (p->n_pages < 1) return fail(h, KV_E_INVAL, "%s: n_pages must be >= 1", call);
-  const int64_t d = c.head_dim, elt = h->cache_elt, most = 1ll << 40;
+  const int64_t d = c.head_dim, elt = h->cache_elt, most = (((1ll << 32) - 1) * 16) / elt;      // (kernels count in 16 bytes, 32 bits)
   if (p->page_stride < d || p->slot_stride < d || p->head_stride < d || p->page_stride > most || p->slot_stride > most || p->head_stride > most)
-    return fail(h, KV_E_INVAL, "%s: strides of the pages must be >= head_dim", call);
+    return fail(h, KV_E_INVAL, "%s: strides of the pages must be >= head_dim and below 2^36 bytes", call);
   if ((((uintptr_t)p->k | (uintptr_t)p->v) & 15) || (p->page_stride * elt) % 16 || (p->slot_stride * elt) % 16 || (p->head_stride * elt) % 16)
     return fail(h, KV_E_INVAL, "%s: rows of the pages must be 16-byte aligned", call);
   if (p->pages_per_seq < 1 || p->table_stride < p->pages_per_seq)
@@ -168,9 +169,9 @@ int check_call(kv_paged* h, const char* call, const kv_pages* p, const kv_paged_
   Call& o = *out;
   o.k = (uint8_t*)p->k;
   o.v = (uint8_t*)p->v;
-  o.page_stride = p->page_stride * elt;
-  o.slot_stride = p->slot_stride * elt;
-  o.head_stride = p->head_stride * elt;
+  o.page_stride = (uint32_t)(p->page_stride * elt / 16);
+  o.slot_stride = (uint32_t)(p->slot_stride * elt / 16);
+  o.head_stride = (uint32_t)(p->head_stride * elt / 16);
   o.table = p->page_table;
   o.table_stride = p->table_stride;
   o.k_scale = p->k_scale;
@@ -212,7 +213,7 @@ void plan_tiles(const kv_paged* h, AttendArgs& a, int tile_rows) {
 // Most keys that a row tile reads.
 int64_t reach(const AttendArgs& a) {
   int64_t keys = a.c.max_len;
-  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + (a.causal ? std::min<int64_t>(a.c.max_new, kChunkRows) : a.c.max_new) + 64);
+  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + (a.causal ? std::min<int64_t>(a.c.max_new, kLargeRows) : a.c.max_new) + 64);
   return align_up(keys, 64);
 }
 
@@ -228,12 +229,19 @@ void plan_workers(const kv_paged* h, AttendArgs& a) {
   a.workers = keys <= 256 || (keys <= 1024 && columns >= 2 * workers) ? 0 : (int32_t)std::min<int64_t>(workers, columns * ((keys + 127) / 128));
 }
 
-// Launches of more rows: key ranges per row tile, for the fewest rounds of two workgroups a compute unit; a workgroup costs about four
-// tiles of 64 keys by itself.
-void plan_splits(const kv_paged* h, AttendArgs& a) {
+// Large tiles halve what is brought into LDS for a row; small ones where the sequences would not fill them.
+bool large_tiles(const kv_paged* h, const AttendArgs& a) {
+  static const char* e = getenv("KVX_L");
+  if (e) return atoi(e);
+  return (int64_t)a.c.n_tokens * h->group >= (int64_t)2 * kLargeRows * a.c.n_seqs;
+}
+
+// Launches of more rows: key ranges per row tile, for the fewest rounds of the workgroups that the chip holds at a time; a workgroup costs
+// about four tiles of 64 keys by itself.
+void plan_splits(const kv_paged* h, AttendArgs& a, int tile_rows) {
   const int64_t keys = reach(a), columns = (int64_t)a.tiles * a.c.hkv;
   const int64_t fit = std::max<int64_t>(1, h->part_rows_cap / std::max<int64_t>(1, columns * a.part_rows));
-  const int64_t slots = 2ll * h->n_cus, tiles = keys / 64;
+  const int64_t slots = (tile_rows == kLargeRows ? 1ll : h->cfg.head_dim == 128 ? 2ll : 3ll) * h->n_cus, tiles = keys / 64;
   int64_t range = keys;
   double best = 0.0;
   for (int64_t s = 1; s <= std::min<int64_t>(16, tiles); ++s) {
@@ -287,7 +295,7 @@ int kv_paged_init(const kv_paged_config* cfg, kv_paged** out) {
   // partial results: two places a worker, and what plan_splits can ask for up to 256 K rows (calls that would need more get fewer ranges)
   const int64_t few_rows = (int64_t)c.n_kv_heads * c.max_seqs * std::min<int64_t>(kFewRows, (int64_t)c.max_tokens * h->group);
   const int64_t chunk_rows = (int64_t)c.max_tokens * h->group > kFewRows
-                                 ? c.n_kv_heads * ((int64_t)c.max_tokens * h->group + (int64_t)kChunkRows * c.max_seqs) : 0;
+                                 ? c.n_kv_heads * ((int64_t)c.max_tokens * h->group + (int64_t)kLargeRows * c.max_seqs) : 0;
   h->part_rows_cap = std::max<int64_t>(2ll * few_workers(h) * std::min<int64_t>(kFewRows, (int64_t)c.max_tokens * h->group),
                                        std::min<int64_t>(1 << 18, chunk_rows * ((c.max_len + 127) / 128)));
   const int64_t part_bytes = h->part_rows_cap * (c.head_dim * 4 + 8);
@@ -379,10 +387,10 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   a.window = std::min(window, 1 << 28);      // no sequence is longer
   if (a.c.n_tokens > 0 && a.c.max_new > 0) {
     const int64_t rows = (int64_t)a.c.max_new * h->group;
-    const int tile_rows = rows <= kFewRows ? kFewRows : kChunkRows;
+    const int tile_rows = rows <= kFewRows ? kFewRows : large_tiles(h, a) ? kLargeRows : kChunkRows;
     plan_tiles(h, a, tile_rows);
     if (tile_rows == kFewRows) plan_workers(h, a);
-    else plan_splits(h, a);
+    else plan_splits(h, a, tile_rows);
     if ((int64_t)a.tiles * a.c.hkv * a.splits > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: too many workgroups");
     // A kept logit is 4 bytes written and 4 read, a key formed again d elements: up to as many rows as make that the same.
     a.logit_stride = align_up(a.c.max_len, 64);

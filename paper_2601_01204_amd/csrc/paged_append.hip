@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
       store8<T>(dst + 2 * c0, x0);
       store8<T>(dst + 2 * c1, x1);
     } else if (page >= 0) {
-      uint8_t* dst = (is_v ? c.v : c.k) + page * c.page_stride + slot * c.slot_stride + kv * c.head_stride;
+      uint8_t* dst = (is_v ? c.v : c.k) + slot_offset(c, page, slot) + head_offset(c, kv);
       if constexpr (E4M3) {
         const float* scales = is_v ? c.v_scale : c.k_scale;
         const float scale = scales ? scales[kv] : 1.0f;

@@ -91,8 +91,8 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     const int all_lo = a.window > 0 ? s.len - a.window : 0;
     const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
 
-    const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
-    const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
+    const uint8_t* const kp = c.k + head_offset(c, head) + 16 * ld_chunk;
+    const uint8_t* const vp = c.v + head_offset(c, head) + 16 * ld_chunk;
     u32x4 rk[kLoads], rv[kLoads];
     uint32_t absent_next = 0;
     int32_t page = -1;
@@ -101,11 +101,11 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
       const uint64_t bad = __ballot(page < 0);
       absent_next = (uint32_t)bad;
       if (bad && lane == 0) note_bad_page(c);
-      const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
+      const uint64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row), slot = (uint64_t)c.slot_stride << 4;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + at + i * c.slot_stride));
-        rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + at + i * c.slot_stride));
+        rk[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + at + i * slot));
+        rv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + at + i * slot));
       }
     };
     // where this lane's row keeps its logits, four keys at a time
@@ -199,18 +199,17 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
   }
 }
 
-// ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
+// ---- more rows: WAVES waves of 32 rows share tiles of 64 keys -----------------------------------------------------
 // Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is d / 4 matrix cycles x 16 (512 for d = 128) and some 290
 // vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
 // before it goes through its exponentials, then the second product of that one.  K is staged two tiles ahead and V one, three tiles of K
-// and two of V in LDS, one barrier a tile; loads are issued half a tile before they are stored.
-constexpr int kChunkRows = 128;
-
-template <typename T, int D, bool E4M3>
-__global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a) {
+// and two of V in LDS, one barrier a tile; loads are issued a tile before they are stored.
+template <typename T, int D, bool E4M3, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const AttendArgs a) {
   typedef Shape<D, E4M3> S;
   constexpr int kRB = S::kRowBytes, kLPR = S::kLanesPerRow;
-  constexpr int kLoads = 64 * kLPR / 256;
+  constexpr int kRows = 32 * WAVES, kLoaders = WAVES < kLPR ? 64 * WAVES : 64 * kLPR;      // threads that bring rows, kLoads pieces of 16 bytes each
+  constexpr int kLoads = 64 * kLPR / kLoaders;
   constexpr int kTile = 64 * kRB;
   __shared__ __align__(16) uint8_t lds[5 * kTile];           // K, K, K, V, V
 
@@ -220,13 +219,13 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   const int column = blockIdx.x % columns, tile = a.tiles - 1 - blockIdx.x / columns;      // long causal tiles first
   const int head = column % c.hkv, split = column / c.hkv;
   int b, t;
-  if (!find_tile(a, tile, kChunkRows, b, t)) return;
+  if (!find_tile(a, tile, kRows, b, t)) return;
   b = uniform(b);
   t = uniform(t);
   const Seq s = uniform(sequence(c, b));
-  const int rows = s.n * c.group, row0 = t * kChunkRows;
+  const int rows = s.n * c.group, row0 = t * kRows;
   if (row0 >= rows) return;
-  const int n_rows = min(kChunkRows, rows - row0);
+  const int n_rows = min(kRows, rows - row0);
   const Range range = tile_range(a, s, row0, n_rows);
   const int n_splits = splits_of(a, range);
   if (split >= n_splits) return;
@@ -247,24 +246,35 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   const int all_lo = uniform(a.window > 0 ? place_last + 1 - a.window : 0), any_lo = uniform(a.window > 0 ? place_first + 1 - a.window : 0);
   const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
 
-  const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR;
-  const uint8_t* const kp = c.k + head * c.head_stride + 16 * ld_chunk;
-  const uint8_t* const vp = c.v + head * c.head_stride + 16 * ld_chunk;
-  u32x4 r[kLoads];                                           // rows on their way: of K and of V in turn
-  int32_t page = 0;                                          // of a tile's keys, one a lane: the tile whose rows are loaded next
+  // A wave brings 8 or 16 neighbouring rows, which lie in one or two pages: their places are scalars but for the lane's own part.
+  constexpr int kWaveRows = kLoads * 64 / kLPR;
+  const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR, slot_mask = (1 << c.page_shift) - 1;
+  const uint64_t slot_bytes = (uint64_t)c.slot_stride << 4, lane_part = (uint64_t)(ld_row & slot_mask) * slot_bytes + 16 * ld_chunk;
+  const uint8_t* const kp = c.k + head_offset(c, head);
+  const uint8_t* const vp = c.v + head_offset(c, head);
+  u32x4 rk[kLoads], rv[kLoads];                              // rows on their way
+  int32_t page_k = 0, page_v = 0;                            // of a tile's keys, one a lane: the tiles of K and of V whose rows are loaded next
   uint64_t absent_loaded = 0;                                // keys without a page: of the tile of V in the registers
-  auto fetch_page = [&](int u) { page = u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
-  auto fetch = [&](const uint8_t* p, int u) {
-    const int64_t at = row_offset(c, __shfl(page, ld_row), u + ld_row);
+  auto page_at = [&](int u) { return u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
+  auto fetch = [&](u32x4 (&r)[kLoads], const uint8_t* p, int32_t page, int u) {
+    if (kLoaders < 64 * WAVES && (int)threadIdx.x >= kLoaders) return;
+    const int first_row = kWaveRows * wave;                  // (u is a multiple of 64: u & slot_mask is 0 in pages of fewer slots)
+    uint64_t at = slot_offset(c, __builtin_amdgcn_readlane(page, first_row), u & slot_mask);
+    if constexpr (kWaveRows == 16) {
+      const uint64_t second = slot_offset(c, __builtin_amdgcn_readlane(page, first_row + 8), u & slot_mask);
+      if (ld_row - first_row >= 8) at = second;
+    }
+    const uint8_t* const q = p + at + lane_part;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) r[i] = *reinterpret_cast<const u32x4*>(p + at + i * c.slot_stride);
+    for (int i = 0; i < kLoads; ++i) r[i] = *reinterpret_cast<const u32x4*>(q + i * slot_bytes);
   };
   auto fetch_v = [&](int u) {
-    absent_loaded = __ballot(page < 0);
+    absent_loaded = __ballot(page_v < 0);
     if (absent_loaded && threadIdx.x == 0) note_bad_page(c);
-    fetch(vp, u);
+    fetch(rv, vp, page_v, u);
   };
-  auto put = [&](int buf) {
+  auto put = [&](const u32x4 (&r)[kLoads], int buf) {
+    if (kLoaders < 64 * WAVES && (int)threadIdx.x >= kLoaders) return;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lds + buf * kTile + lds_offset<kRB>(ld_row + i, ld_chunk)) = r[i];
   };
@@ -272,27 +282,30 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
     if (u + 64 > s.len || absent_loaded)
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
-        if (u + ld_row + i >= s.len || ((absent_loaded >> (ld_row + i)) & 1)) r[i] = (u32x4){0, 0, 0, 0};
-    put(3 + buf);
+        if (u + ld_row + i >= s.len || ((absent_loaded >> (ld_row + i)) & 1)) rv[i] = (u32x4){0, 0, 0, 0};
+    put(rv, 3 + buf);
   };
   auto live = [&](int key0) { return key0 < k1 && key0 < any_hi && key0 + 32 > any_lo; };
 
-  // in LDS before the first tile: its K and V and the next one's K; on the way: the next one's V
+  // in LDS before the first tile: its K and V and the next one's K; on the way: the next one's V and the third one's K
   uint64_t absent = 0;                                       // of the running tile
   f32x16 x, y;                                               // logits of the running unit, then its probabilities; of the next one
   if (k0 < k1) {
-    fetch_page(k0);
-    fetch(kp, k0);
-    put(0);
+    page_v = page_at(k0);
+    fetch(rk, kp, page_v, k0);
     fetch_v(k0);
+    page_k = page_at(k0 + 64);
+    put(rk, 0);
     put_v(0, k0);
     absent = absent_loaded;
-    fetch_page(k0 + 64);
     if (k0 + 64 < k1) {
-      fetch(kp, k0 + 64);
-      put(1);
+      fetch(rk, kp, page_k, k0 + 64);
+      page_v = page_k;
       fetch_v(k0 + 64);
-      fetch_page(k0 + 128);
+      page_v = page_at(k0 + 128);
+      put(rk, 1);
+      if (k0 + 128 < k1) fetch(rk, kp, page_v, k0 + 128);
+      page_k = page_at(k0 + 192);
     }
   }
   __syncthreads();
@@ -331,11 +344,12 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
           put_v(vb ^ 1, u + 64);
           absent_next = absent_loaded;
         }
-        if (u + 128 < k1) fetch(kp, u + 128);
+        if (u + 128 < k1) fetch_v(u + 128);
       } else if (u + 128 < k1) {
-        put(kb2);
-        fetch_v(u + 128);
-        fetch_page(u + 192);
+        put(rk, kb2);
+        if (u + 192 < k1) fetch(rk, kp, page_k, u + 192);
+        page_v = page_k;
+        page_k = page_at(u + 256);
       }
     }
     __syncthreads();
@@ -487,7 +501,8 @@ void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_ro
   by_type(d, dtype, e4m3, [&](auto t, auto dd, auto f8) {
     if (tile_rows == 32 && a.part_rows <= 16) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 16><<<grid, dim3(256), 0, st>>>(a);
     else if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 32><<<grid, dim3(256), 0, st>>>(a);
-    else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
+    else if (tile_rows == 128) attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 4><<<grid, dim3(256), 0, st>>>(a);
+    else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 8><<<grid, dim3(512), 0, st>>>(a);
   });
 }
 

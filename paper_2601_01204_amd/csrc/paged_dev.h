@@ -11,11 +11,11 @@ struct Rows {                   // strides in bytes
   int64_t tok, head;
 };
 
-// One call's geometry; strides of the pool in bytes.
+// One call's geometry.
 struct Call {
   uint8_t* k;
   uint8_t* v;
-  int64_t page_stride, slot_stride, head_stride;
+  uint32_t page_stride, slot_stride, head_stride;      // of the pool, in pieces of 16 bytes
   const int32_t* table;
   int64_t table_stride;
   const float* k_scale;

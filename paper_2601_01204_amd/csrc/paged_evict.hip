@@ -40,8 +40,8 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int head, c
     const int2 m = moves[i];
     const int32_t from = page_of(c, b, m.x >> c.page_shift), to = page_of(c, b, m.y >> c.page_shift);
     if (from < 0 || to < 0) continue;                                // (a token without a page never stays unless the budget asks for it)
-    const int64_t src = from * c.page_stride + (m.x & mask) * c.slot_stride + head * c.head_stride + 16 * chunk;
-    const int64_t dst = to * c.page_stride + (m.y & mask) * c.slot_stride + head * c.head_stride + 16 * chunk;
+    const uint64_t src = slot_offset(c, from, m.x & mask) + head_offset(c, head) + 16 * chunk;
+    const uint64_t dst = slot_offset(c, to, m.y & mask) + head_offset(c, head) + 16 * chunk;
     const u32x4 k = *reinterpret_cast<const u32x4*>(c.k + src), v = *reinterpret_cast<const u32x4*>(c.v + src);
     *reinterpret_cast<u32x4*>(c.k + dst) = k;
     *reinterpret_cast<u32x4*>(c.v + dst) = v;

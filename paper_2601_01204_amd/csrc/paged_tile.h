@@ -354,9 +354,7 @@ struct FewRows {
 __device__ __forceinline__ int32_t page_of_key(const Call& c, int b, int key, int len) {
   return page_of(c, b, min(key, len - 1) >> c.page_shift);
 }
-__device__ __forceinline__ int64_t row_offset(const Call& c, int32_t page, int key) {
-  return (page < 0 ? 0 : page) * c.page_stride + (int64_t)(key & ((1 << c.page_shift) - 1)) * c.slot_stride;
-}
+__device__ __forceinline__ uint64_t row_offset(const Call& c, int32_t page, int key) { return slot_offset(c, page, key & ((1 << c.page_shift) - 1)); }
 
 // Which rows a workgroup works on: row tile `t` of sequence `b`; false: none.
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, int tile, int tile_rows, int& b, int& t) {

@@ -84,6 +84,12 @@ __device__ __forceinline__ int32_t page_of(const Call& c, int b, int entry) {
   const int32_t page = c.table[(int64_t)b * c.table_stride + entry];
   return (uint32_t)page < (uint32_t)c.n_pages ? page : -1;
 }
+// Bytes from the pool's beginning to a slot of a page (0 for a page outside the pool) and a key head: 32 x 32-bit products, since 64-bit ones
+// take a wave a hundred cycles.
+__device__ __forceinline__ uint64_t slot_offset(const Call& c, int32_t page, int slot) {
+  return ((uint64_t)(uint32_t)(page < 0 ? 0 : page) * c.page_stride + (uint64_t)(uint32_t)slot * c.slot_stride) << 4;
+}
+__device__ __forceinline__ uint64_t head_offset(const Call& c, int head) { return ((uint64_t)(uint32_t)head * c.head_stride) << 4; }
 __device__ __forceinline__ void note_bad_page(const Call& c) { atomicOr(c.status, kStatusPage); }
 // The sequence that row t belongs to (-1: none), found by all lanes of a wave together; t is the same in all of them.
 // Sequences with no rows are passed over: the answer is the last one that begins at or before t.

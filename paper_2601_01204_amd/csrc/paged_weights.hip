@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
 
   u32x4 kf[kSteps];
   {
-    const uint8_t* kp = c.k + head * c.head_stride + row_offset(c, page, key);
+    const uint8_t* kp = c.k + head_offset(c, head) + row_offset(c, page, key);
     if constexpr (E4M3) {
 #pragma unroll
       for (int i = 0; i < kSteps / 2; ++i) {

@@ -39,7 +39,7 @@ void launch_attend(const AttendArgs& a, int d, int, bool, int tile_rows, hipStre
   CHECK(a.tiles >= std::min<int64_t>(per_seq * a.c.n_seqs, (int64_t)a.c.n_tokens * a.c.group / tile_rows + a.c.n_seqs));
   const int64_t reach = a.window > 0 ? std::min<int64_t>(a.c.max_len, (int64_t)a.window + 63 + (a.causal ? std::min(a.c.max_new, tile_rows) : a.c.max_new)) : a.c.max_len;
   CHECK((int64_t)a.splits * a.split_keys >= reach);
-  CHECK(a.workers >= 0 && (!a.workers || (tile_rows == 32 && a.splits == 1)) && (tile_rows == 128 || a.tiles == a.c.n_seqs));
+  CHECK(a.workers >= 0 && (!a.workers || (tile_rows == 32 && a.splits == 1)) && (tile_rows != 32 || a.tiles == a.c.n_seqs));
   if (a.splits > 1 || a.workers) {
     const int64_t rows = (a.workers ? 2ll * a.workers : (int64_t)a.tiles * a.c.hkv * a.splits) * a.part_rows;
     a.part_o[0] = a.part_o[rows * d - 1] = 1.f;
