@@ -7,7 +7,6 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
-#include <cstdlib>
 #include <new>
 #include <string>
 #include <vector>
@@ -56,7 +55,7 @@ int fail(kv_paged* h, int code, const char* fmt, ...) {
 
 int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kFewRows = 32, kChunkRows = 128, kLargeRows = 256;      // row tiles of the attention kernels
+constexpr int kFewRows = 32, kChunkRows = 128;      // row tiles of the attention kernels
 
 int check_config(const kv_paged_config* c) {
   if (!c) return fail(nullptr, KV_E_INVAL, "kv_paged_init: cfg is NULL");
@@ -213,7 +212,7 @@ void plan_tiles(const kv_paged* h, AttendArgs& a, int tile_rows) {
 // Most keys that a row tile reads.
 int64_t reach(const AttendArgs& a) {
   int64_t keys = a.c.max_len;
-  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + (a.causal ? std::min<int64_t>(a.c.max_new, kLargeRows) : a.c.max_new) + 64);
+  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + (a.causal ? std::min<int64_t>(a.c.max_new, kChunkRows) : a.c.max_new) + 64);
   return align_up(keys, 64);
 }
 
@@ -229,19 +228,12 @@ void plan_workers(const kv_paged* h, AttendArgs& a) {
   a.workers = keys <= 256 || (keys <= 1024 && columns >= 2 * workers) ? 0 : (int32_t)std::min<int64_t>(workers, columns * ((keys + 127) / 128));
 }
 
-// Large tiles halve what is brought into LDS for a row; small ones where the sequences would not fill them.
-bool large_tiles(const kv_paged* h, const AttendArgs& a) {
-  static const char* e = getenv("KVX_L");
-  if (e) return atoi(e);
-  return (int64_t)a.c.n_tokens * h->group >= (int64_t)2 * kLargeRows * a.c.n_seqs;
-}
-
 // Launches of more rows: key ranges per row tile, for the fewest rounds of the workgroups that the chip holds at a time; a workgroup costs
 // about four tiles of 64 keys by itself.
-void plan_splits(const kv_paged* h, AttendArgs& a, int tile_rows) {
+void plan_splits(const kv_paged* h, AttendArgs& a) {
   const int64_t keys = reach(a), columns = (int64_t)a.tiles * a.c.hkv;
   const int64_t fit = std::max<int64_t>(1, h->part_rows_cap / std::max<int64_t>(1, columns * a.part_rows));
-  const int64_t slots = (tile_rows == kLargeRows ? 1ll : h->cfg.head_dim == 128 ? 2ll : 3ll) * h->n_cus, tiles = keys / 64;
+  const int64_t slots = (h->cfg.head_dim == 128 ? 2ll : 3ll) * h->n_cus, tiles = keys / 64;
   int64_t range = keys;
   double best = 0.0;
   for (int64_t s = 1; s <= std::min<int64_t>(16, tiles); ++s) {
@@ -295,7 +287,7 @@ int kv_paged_init(const kv_paged_config* cfg, kv_paged** out) {
   // partial results: two places a worker, and what plan_splits can ask for up to 256 K rows (calls that would need more get fewer ranges)
   const int64_t few_rows = (int64_t)c.n_kv_heads * c.max_seqs * std::min<int64_t>(kFewRows, (int64_t)c.max_tokens * h->group);
   const int64_t chunk_rows = (int64_t)c.max_tokens * h->group > kFewRows
-                                 ? c.n_kv_heads * ((int64_t)c.max_tokens * h->group + (int64_t)kLargeRows * c.max_seqs) : 0;
+                                 ? c.n_kv_heads * ((int64_t)c.max_tokens * h->group + (int64_t)kChunkRows * c.max_seqs) : 0;
   h->part_rows_cap = std::max<int64_t>(2ll * few_workers(h) * std::min<int64_t>(kFewRows, (int64_t)c.max_tokens * h->group),
                                        std::min<int64_t>(1 << 18, chunk_rows * ((c.max_len + 127) / 128)));
   const int64_t part_bytes = h->part_rows_cap * (c.head_dim * 4 + 8);
@@ -387,10 +379,10 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   a.window = std::min(window, 1 << 28);      // no sequence is longer
   if (a.c.n_tokens > 0 && a.c.max_new > 0) {
     const int64_t rows = (int64_t)a.c.max_new * h->group;
-    const int tile_rows = rows <= kFewRows ? kFewRows : large_tiles(h, a) ? kLargeRows : kChunkRows;
+    const int tile_rows = rows <= kFewRows ? kFewRows : kChunkRows;
     plan_tiles(h, a, tile_rows);
     if (tile_rows == kFewRows) plan_workers(h, a);
-    else plan_splits(h, a, tile_rows);
+    else plan_splits(h, a);
     if ((int64_t)a.tiles * a.c.hkv * a.splits > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: too many workgroups");
     // A kept logit is 4 bytes written and 4 read, a key formed again d elements: up to as many rows as make that the same.
     a.logit_stride = align_up(a.c.max_len, 64);
@@ -400,7 +392,7 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
     a.part_o = (float*)h->work;
     a.part_ml = (float2*)(h->work + h->part_rows_cap * c.head_dim * 4);
     launch_attend(a, c.head_dim, c.dtype, e4m3, tile_rows, st);
-    if (a.splits > 1 || a.workers) launch_merge(a, c.head_dim, c.dtype, tile_rows, e4m3, st);
+    if (a.splits > 1 || a.workers) launch_merge(a, c.head_dim, c.dtype, e4m3, st);
   }
   if (a.logits) launch_weights_from_logits(a, st);
   else if (weights_out) launch_weights(a, c.head_dim, c.dtype, e4m3, st);

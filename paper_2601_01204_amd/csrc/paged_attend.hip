@@ -199,17 +199,18 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
   }
 }
 
-// ---- more rows: WAVES waves of 32 rows share tiles of 64 keys -----------------------------------------------------
+// ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
 // Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is d / 4 matrix cycles x 16 (512 for d = 128) and some 290
 // vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
 // before it goes through its exponentials, then the second product of that one.  K is staged two tiles ahead and V one, three tiles of K
 // and two of V in LDS, one barrier a tile; loads are issued a tile before they are stored.
-template <typename T, int D, bool E4M3, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const AttendArgs a) {
+constexpr int kChunkRows = 128;
+
+template <typename T, int D, bool E4M3>
+__global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a) {
   typedef Shape<D, E4M3> S;
   constexpr int kRB = S::kRowBytes, kLPR = S::kLanesPerRow;
-  constexpr int kRows = 32 * WAVES, kLoaders = WAVES < kLPR ? 64 * WAVES : 64 * kLPR;      // threads that bring rows, kLoads pieces of 16 bytes each
-  constexpr int kLoads = 64 * kLPR / kLoaders;
+  constexpr int kLoads = 64 * kLPR / 256;
   constexpr int kTile = 64 * kRB;
   __shared__ __align__(16) uint8_t lds[5 * kTile];           // K, K, K, V, V
 
@@ -219,13 +220,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const Atten
   const int column = blockIdx.x % columns, tile = a.tiles - 1 - blockIdx.x / columns;      // long causal tiles first
   const int head = column % c.hkv, split = column / c.hkv;
   int b, t;
-  if (!find_tile(a, tile, kRows, b, t)) return;
+  if (!find_tile(a, tile, kChunkRows, b, t)) return;
   b = uniform(b);
   t = uniform(t);
   const Seq s = uniform(sequence(c, b));
-  const int rows = s.n * c.group, row0 = t * kRows;
+  const int rows = s.n * c.group, row0 = t * kChunkRows;
   if (row0 >= rows) return;
-  const int n_rows = min(kRows, rows - row0);
+  const int n_rows = min(kChunkRows, rows - row0);
   const Range range = tile_range(a, s, row0, n_rows);
   const int n_splits = splits_of(a, range);
   if (split >= n_splits) return;
@@ -246,8 +247,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const Atten
   const int all_lo = uniform(a.window > 0 ? place_last + 1 - a.window : 0), any_lo = uniform(a.window > 0 ? place_first + 1 - a.window : 0);
   const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
 
-  // A wave brings 8 or 16 neighbouring rows, which lie in one or two pages: their places are scalars but for the lane's own part.
-  constexpr int kWaveRows = kLoads * 64 / kLPR;
+  // A wave brings 16 neighbouring rows, which lie in one or two pages: their places are scalars but for the lane's own part.
   const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR, slot_mask = (1 << c.page_shift) - 1;
   const uint64_t slot_bytes = (uint64_t)c.slot_stride << 4, lane_part = (uint64_t)(ld_row & slot_mask) * slot_bytes + 16 * ld_chunk;
   const uint8_t* const kp = c.k + head_offset(c, head);
@@ -257,14 +257,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const Atten
   uint64_t absent_loaded = 0;                                // keys without a page: of the tile of V in the registers
   auto page_at = [&](int u) { return u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
   auto fetch = [&](u32x4 (&r)[kLoads], const uint8_t* p, int32_t page, int u) {
-    if (kLoaders < 64 * WAVES && (int)threadIdx.x >= kLoaders) return;
-    const int first_row = kWaveRows * wave;                  // (u is a multiple of 64: u & slot_mask is 0 in pages of fewer slots)
-    uint64_t at = slot_offset(c, __builtin_amdgcn_readlane(page, first_row), u & slot_mask);
-    if constexpr (kWaveRows == 16) {
-      const uint64_t second = slot_offset(c, __builtin_amdgcn_readlane(page, first_row + 8), u & slot_mask);
-      if (ld_row - first_row >= 8) at = second;
-    }
-    const uint8_t* const q = p + at + lane_part;
+    const int first_row = 16 * wave;                         // (u is a multiple of 64: u & slot_mask is 0 in pages of fewer slots)
+    const uint64_t low = slot_offset(c, __builtin_amdgcn_readlane(page, first_row), u & slot_mask);
+    const uint64_t high = slot_offset(c, __builtin_amdgcn_readlane(page, first_row + 8), u & slot_mask);
+    const uint8_t* const q = p + (ld_row - first_row < 8 ? low : high) + lane_part;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) r[i] = *reinterpret_cast<const u32x4*>(q + i * slot_bytes);
   };
@@ -274,7 +270,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const Atten
     fetch(rv, vp, page_v, u);
   };
   auto put = [&](const u32x4 (&r)[kLoads], int buf) {
-    if (kLoaders < 64 * WAVES && (int)threadIdx.x >= kLoaders) return;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lds + buf * kTile + lds_offset<kRB>(ld_row + i, ld_chunk)) = r[i];
   };
@@ -333,7 +328,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const Atten
           sum = w.template soften<false>(x, factor, k_next, lane, y);
         }
         w.l += sum;
+        __builtin_amdgcn_s_setprio(1);                       // (the matrix cores before the other wave's exponentials)
         w.add_values(x, v_now, lane);
+        __builtin_amdgcn_s_setprio(0);
       } else if (next) {
         y = w.logits(k_next, lane);
       }
@@ -382,54 +379,38 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attend_chunk_kernel(const Atten
   }
 }
 
-// ---- partial results of a row's key ranges ------------------------------------------------------------------------------
-// WAVES waves join one row (token, query head): a lane has four channels, 256 / D lane groups of a wave take a range each and the
-// next ranges after it, four loads ahead.  One wave is enough for a few ranges; 128 of them took one wave 58 us (128 rows, d = 128,
-// two channels a lane, one range after the other).
+// ---- partial results ------------------------------------------------------------------------------------------------
+// Launches of few rows: WAVES waves join the pieces of one row (token, query head).  A lane has four channels, 256 / D lane groups of a wave
+// take a piece each and the next ones after it, four loads ahead.  One wave is enough for a few pieces; 128 of them took one wave 58 us
+// (128 rows, d = 128, two channels a lane, one piece after the other).
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const int tile_rows, const bool scaled) {
+__global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const bool scaled) {
   constexpr int kLanes = D / 4, kGroups = 64 / kLanes * WAVES;      // lanes of a range, ranges at a time
   __shared__ float join[WAVES > 1 ? WAVES : 1][D + 1];
   const Call& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t job = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
-  const int token = (int)(job / c.hq), qh = (int)(job - (int64_t)token * c.hq);
+  const uint32_t job = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  const int token = (int)(job / (uint32_t)c.hq), qh = (int)(job - (uint32_t)token * (uint32_t)c.hq);
   if (token >= c.n_tokens) return;
   const int head = qh / c.group;
-  int64_t first;                                             // the first piece's place among the pieces of part_rows rows each
-  int n, apart = 1, row;                                     // how many, and from one to the next; the row within its sequence
-  if (a.workers) {
-    // a worker's places: 0 for a column that began before it, 1 for one that ends behind it, so the first piece lies in a 1, others in a 0
-    int before = 0, units = -1, in_front = 0;
-    for (int base = 0; base < c.n_seqs; base += 64) {
-      const Lanes x = load_lanes(a, base, before);
-      const uint64_t mine = __ballot(token >= x.mine.first && token < x.mine.first + x.mine.n);
-      if (units < 0 && mine) {
-        const int at = __ffsll((unsigned long long)mine) - 1;
-        units = __shfl(x.units, at);
-        in_front = before + __shfl(x.upto, at) - units;
-        row = (token - __shfl(x.mine.first, at)) * c.group + qh - head * c.group;
-      }
-      before += x.all;
+  int before = 0, units = -1, in_front = 0, row = 0;
+  for (int base = 0; base < c.n_seqs; base += 64) {
+    const Lanes x = load_lanes(a, base, before);
+    const uint64_t mine = __ballot(token >= x.mine.first && token < x.mine.first + x.mine.n);
+    if (units < 0 && mine) {
+      const int at = __ffsll((unsigned long long)mine) - 1;
+      units = __shfl(x.units, at);
+      in_front = before + __shfl(x.upto, at) - units;
+      row = (token - __shfl(x.mine.first, at)) * c.group + qh - head * c.group;
     }
-    if (units < 0) return;
-    const int begin = in_front * c.hkv + head * units, share = share_of(a, before * c.hkv), w0 = begin / share;
-    n = units ? (begin + units - 1) / share - w0 + 1 : 0;
-    first = (int64_t)w0 * 2;
-    apart = 2;
-  } else {
-    const int b = sequence_of_row(c, token);
-    if (b < 0) return;
-    const Seq s = sequence(c, b);
-    const int i_row = token - s.first;
-    if (i_row < 0 || i_row >= s.n) return;
-    row = i_row * c.group + qh - head * c.group;
-    const int t = row / tile_rows, row0 = t * tile_rows;
-    n = splits_of(a, tile_range(a, s, row0, min(tile_rows, s.n * c.group - row0)));
-    first = ((int64_t)tile_number(a, b, t, tile_rows) * c.hkv + head) * a.splits;
+    before += x.all;
   }
+  if (units < 0) return;
+  // A worker's places: 0 for a column that began before it, 1 for one that ends behind it, so the first piece lies in a 1, others in a 0.
+  const int begin = in_front * c.hkv + head * units, share = share_of(a, before * c.hkv), w0 = begin / share;
+  const int n = units ? (begin + units - 1) / share - w0 + 1 : 0;      // 0: the row sees nothing
   if (n == 1) return;                                        // written already
-  auto piece = [&](int i) { return (first + (int64_t)i * apart + (apart == 2 && i == 0 ? 1 : 0)) * a.part_rows + row % tile_rows; };
+  auto piece = [&](int i) { return ((int64_t)(w0 + i) * 2 + (i == 0 ? 1 : 0)) * a.part_rows + row; };
   float m = -kInf;
   for (int i = lane; i < n; i += 64) m = fmaxf(m, a.part_ml[piece(i)].x);
 #pragma unroll
@@ -480,6 +461,48 @@ __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const in
   if (a.lse && lane == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(m, l);
 }
 
+// Launches of more rows: D / 4 lanes a row of a row tile.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void merge_tile_kernel(const AttendArgs a, const int slices, const bool scaled) {
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+  const Call& c = a.c;
+  const int job = blockIdx.x / slices, slice = blockIdx.x - job * slices, tile = job / c.hkv, head = job - tile * c.hkv;
+  int b, t;
+  if (!find_tile(a, tile, kChunkRows, b, t)) return;
+  b = uniform(b);
+  t = uniform(t);
+  const Seq s = uniform(sequence(c, b));
+  const int row0 = t * kChunkRows, n_rows = min(kChunkRows, s.n * c.group - row0), r = slice * kRows + (int)threadIdx.x / kLanes;
+  if (n_rows <= 0) return;
+  const int n = splits_of(a, tile_range(a, s, row0, n_rows));
+  if (n == 1 || r >= n_rows) return;                         // (one range: written already)
+  const int ch = threadIdx.x % kLanes * 4;
+  const int64_t first = (int64_t)job * a.splits * a.part_rows + r;
+  float m = -kInf;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) m = fmaxf(m, a.part_ml[first + (int64_t)i * a.part_rows].x);
+  const float ref = m == -kInf ? 0.f : m;
+  float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const int64_t at = first + (int64_t)i * a.part_rows;
+    const float2 w = a.part_ml[at];
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + at * D + ch);
+    const float f = __builtin_amdgcn_exp2f(w.x - ref);
+    l += f * w.y;
+    x[0] += f * y.x;
+    x[1] += f * y.y;
+    x[2] += f * y.z;
+    x[3] += f * y.w;
+  }
+  const int row = row0 + r, i_row = row / c.group, token = s.first + i_row, qh = head * c.group + row - i_row * c.group;
+  const float f = l == 0.f ? 0.f : (scaled && c.v_scale ? c.v_scale[head] : 1.f) / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= f;
+  store_out<T>(a, token, qh, ch, x);
+  if (a.lse && ch == 0) a.lse[(int64_t)token * c.hq + qh] = log_sum(m, l);
+}
+
 template <typename F>
 void by_type(int d, int dtype, bool e4m3, F&& f) {
   auto by_d = [&](auto t, auto f8) {
@@ -501,16 +524,23 @@ void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_ro
   by_type(d, dtype, e4m3, [&](auto t, auto dd, auto f8) {
     if (tile_rows == 32 && a.part_rows <= 16) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 16><<<grid, dim3(256), 0, st>>>(a);
     else if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 32><<<grid, dim3(256), 0, st>>>(a);
-    else if (tile_rows == 128) attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 4><<<grid, dim3(256), 0, st>>>(a);
-    else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 8><<<grid, dim3(512), 0, st>>>(a);
+    else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
   });
 }
 
-void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m3, hipStream_t st) {
+void launch_merge(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st) {
   const int64_t rows = (int64_t)a.c.n_tokens * a.c.hq;
   by_type(d, dtype, false, [&](auto t, auto dd, auto) {
-    if (a.workers ? rows * 8 < a.workers : a.splits > 8) merge_kernel<decltype(t), decltype(dd)::value, 4><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a, tile_rows, e4m3);
-    else merge_kernel<decltype(t), decltype(dd)::value, 1><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st>>>(a, tile_rows, e4m3);
+    typedef decltype(t) Type;
+    constexpr int kD = decltype(dd)::value;
+    if (a.workers == 0) {
+      const int slices = (a.part_rows + 1024 / kD - 1) / (1024 / kD);
+      merge_tile_kernel<Type, kD><<<dim3((unsigned)((int64_t)a.tiles * a.c.hkv * slices)), dim3(256), 0, st>>>(a, slices, e4m3);
+    } else if (rows * 8 < a.workers) {
+      merge_kernel<Type, kD, 4><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a, e4m3);
+    } else {
+      merge_kernel<Type, kD, 1><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st>>>(a, e4m3);
+    }
   });
 }
 

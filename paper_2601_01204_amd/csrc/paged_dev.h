@@ -77,7 +77,7 @@ struct EvictArgs {
 // dtype: KV_BF16 or KV_F16; e4m3: the pages hold 8-bit floats.
 void launch_append(const AppendArgs& a, int d, int dtype, bool e4m3, bool interleaved, hipStream_t st);
 void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_rows, hipStream_t st);
-void launch_merge(const AttendArgs& a, int d, int dtype, int tile_rows, bool e4m3, hipStream_t st);
+void launch_merge(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st);
 void launch_weights_from_logits(const AttendArgs& a, hipStream_t st);
 void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st);
 // arrived: [n_seqs], zero before and after

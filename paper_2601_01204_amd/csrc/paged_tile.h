@@ -387,21 +387,6 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int tile, int til
   }
   return false;
 }
-// The tile number of row tile t of sequence b (what find_tile inverts).
-__device__ __forceinline__ int tile_number(const AttendArgs& a, int b, int t, int tile_rows) {
-  if (a.tiles_per_seq > 0) return b * a.tiles_per_seq + t;
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int base = 0; base < b; base += 64) {
-    const int s = base + lane;
-    int mine = s < b ? (sequence(a.c, s).n * a.c.group + tile_rows - 1) / tile_rows : 0;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) mine += __shfl_xor(mine, o);
-    before += mine;
-  }
-  return before + t;
-}
-
 // The keys that row tile t of a sequence reads: [lo, hi), lo on a multiple of 64.
 struct Range {
   int lo, hi;

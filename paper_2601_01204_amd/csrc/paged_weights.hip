@@ -5,7 +5,7 @@
 // read, where K would be another d elements.  weights_kernel forms them again.
 //
 // weights_kernel.  A workgroup owns 128 keys of one key head, a wave 32 of them, whose fragments stay in registers, and goes over all rows that see
-// them, 32 at a time, brought into LDS for the four waves.  S = Q K^T with a key in a lane and its rows in that lane's registers: a key's
+// them, 64 at a time, brought into LDS for the four waves.  S = Q K^T with a key in a lane and its rows in that lane's registers: a key's
 // weights are summed in its lane, in row order, in fp32 without a rounding between, and no two workgroups write the same
 // token, so the sums do not depend on what ran when.
 #include "../../include/kvx.h"
@@ -16,22 +16,22 @@ namespace paged {
 
 namespace {
 
-constexpr int kKeys = 128;
+constexpr int kKeys = 128, kRows = 64;
 
 template <typename T, int D, bool E4M3>
 __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   constexpr int kRB = 2 * D, kLPR = kRB / 16, kSteps = D / 16;     // rows of queries are 16-bit
-  constexpr int kLoads = 32 * kLPR / 256;
-  __shared__ __align__(16) uint8_t lq[2][32 * kRB];
-  __shared__ __align__(16) float l_lse[2][32];                     // log2 units; infinite: the row counts nothing
-  __shared__ __align__(16) int l_hi[2][32], l_lo[2][32];
+  constexpr int kLoads = kRows * kLPR / 256;
+  __shared__ __align__(16) uint8_t lq[2][kRows * kRB];
+  __shared__ __align__(16) float l_lse[2][kRows];                  // log2 units; infinite: the row counts nothing
+  __shared__ __align__(16) int l_place[2][kRows];
 
   const Call& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int key_blocks = (c.max_len + kKeys - 1) / kKeys;
   const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
   const int block = rest % key_blocks, b = rest / key_blocks;
-  const Seq s = sequence(c, b);
+  const Seq s = uniform(sequence(c, b));
   const int kb = block * kKeys;
   if (kb >= s.len) return;
   const int key = kb + 32 * wave + (lane & 31);
@@ -59,70 +59,98 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   const int base = s.len - s.n;
   const int i0 = a.causal ? min(s.n, max(0, kb - base)) : 0;
   const int i1 = a.window > 0 ? max(i0, min(s.n, kb + kKeys - 1 + a.window - base)) : s.n;
-  const int r0 = i0 * c.group, r1 = i1 * c.group;
-  const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR;
+  const int r0 = uniform(i0 * c.group), r1 = uniform(i1 * c.group);
+  // A thread brings the same rows of every kRows: their tokens and heads move on by the same steps (a division by the group would cost more
+  // than a row's exponentials).
+  struct Place {
+    int it, g;
+  };
+  const int step_it = kRows / c.group, step_g = kRows - step_it * c.group;
+  auto place_of = [&](int row) {
+    const int it = row / c.group;
+    return Place{it, row - it * c.group};
+  };
+  auto move_on = [&](Place& x) {
+    x.it += step_it;
+    x.g += step_g;
+    if (x.g >= c.group) {
+      x.g -= c.group;
+      ++x.it;
+    }
+  };
+  const int ld_row = threadIdx.x / kLPR, ld_chunk = threadIdx.x % kLPR;      // and every (256 / kLPR)-th row after it
   u32x4 rq[kLoads];
   float r_lse = 0.f;
-  int r_hi = 0, r_lo = 0;
-  auto fetch = [&](int r) {
+  int r_place = 0;
+  Place at[kLoads], mine = place_of(r0 + (int)(threadIdx.x & (kRows - 1)));
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) at[i] = place_of(r0 + ld_row + i * (256 / kLPR));
+  auto fetch = [&]() {                                             // the next kRows rows; rows behind the last repeat it and count nothing
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int row = min(r + ld_row + i, r1 - 1), it = row / c.group, g = row - it * c.group;
+      const bool real = at[i].it < i1;
+      const int it = real ? at[i].it : i1 - 1, g = real ? at[i].g : c.group - 1;
       rq[i] = *reinterpret_cast<const u32x4*>(a.q.p + (int64_t)(s.first + it) * a.q.tok + (int64_t)(head * c.group + g) * a.q.head + 16 * ld_chunk);
+      move_on(at[i]);
     }
-    if (threadIdx.x < 32) {
-      const int row = min(r + (int)threadIdx.x, r1 - 1), it = row / c.group, g = row - it * c.group;
+    if (threadIdx.x < kRows) {
+      const bool real = mine.it < i1;
+      const int it = real ? mine.it : i1 - 1, g = real ? mine.g : c.group - 1;
       const float x = a.lse[(int64_t)(s.first + it) * c.hq + head * c.group + g];
-      r_lse = r + (int)threadIdx.x >= r1 || x == -kInf ? kInf : x * 1.4426950408889634f;
-      r_hi = a.causal ? min(s.len, base + it + 1) : s.len;
-      r_lo = a.window > 0 ? base + it + 1 - a.window : 0;
+      r_lse = !real || x == -kInf ? kInf : x * 1.4426950408889634f;
+      r_place = base + it;
+      move_on(mine);
     }
   };
   auto put = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lq[buf] + lds_offset<kRB>(ld_row + i, ld_chunk)) = rq[i];
-    if (threadIdx.x < 32) {
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lq[buf] + lds_offset<kRB>(ld_row + i * (256 / kLPR), ld_chunk)) = rq[i];
+    if (threadIdx.x < kRows) {
       l_lse[buf][threadIdx.x] = r_lse;
-      l_hi[buf][threadIdx.x] = r_hi;
-      l_lo[buf][threadIdx.x] = r_lo;
+      l_place[buf][threadIdx.x] = r_place;
     }
   };
   float sum = 0.f;
   if (r0 < r1) {
-    fetch(r0);
+    fetch();
     put(0);
-    if (r0 + 32 < r1) fetch(r0 + 32);
+    if (r0 + kRows < r1) fetch();
   }
   __syncthreads();
   int buf = 0;
-  for (int r = r0; r < r1; r += 32, buf ^= 1) {
-    f32x16 x;
+  // rows from here on see all of the workgroup's keys, and before there
+  const int all_from = a.causal ? uniform(min(s.n, kb + kKeys - 1 - base) * c.group) : 0;
+  const int all_to = a.window > 0 ? uniform(min(s.n, kb + a.window - base) * c.group) : r1 + kRows;
+  for (int r = r0; r < r1; r += kRows, buf ^= 1) {
+    const bool masked = r < all_from || min(r + kRows, r1) > all_to;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = 0.f;
+    for (int half = 0; half < kRows / 32; ++half) {
+      f32x16 x{};
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-      x = T::mfma(*reinterpret_cast<const u32x4*>(lq[buf] + lds_offset<kRB>(lane & 31, step_channel<E4M3>(i, h) / 8)), kf[i], x);
-    const int first = r / c.group, last = (min(r + 32, r1) - 1) / c.group;
-    const bool masked = (a.causal && kb + kKeys > base + first + 1) || (a.window > 0 && kb < base + last + 1 - a.window);
+      for (int i = 0; i < kSteps; ++i)
+        x = T::mfma(*reinterpret_cast<const u32x4*>(lq[buf] + 32 * half * kRB + lds_offset<kRB>(lane & 31, step_channel<E4M3>(i, h) / 8)), kf[i], x);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int at = 8 * g + 4 * h;
-      const float4 l4 = *reinterpret_cast<const float4*>(&l_lse[buf][at]);
-      const float ls[4] = {l4.x, l4.y, l4.z, l4.w};
-      if (masked) {
+      for (int g = 0; g < 4; ++g) {
+        const int first = 32 * half + 8 * g + 4 * h;
+        const float4 l4 = *reinterpret_cast<const float4*>(&l_lse[buf][first]);
+        const float ls[4] = {l4.x, l4.y, l4.z, l4.w};
+        if (masked) {
+          const int4 p4 = *reinterpret_cast<const int4*>(&l_place[buf][first]);
+          const int place[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + e], factor, -ls[e]));
-          sum += key < l_hi[buf][at + e] && key >= l_lo[buf][at + e] ? p : 0.f;
+          for (int e = 0; e < 4; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + e], factor, -ls[e]));
+            sum += (!a.causal || key <= place[e]) && (a.window == 0 || key > place[e] - a.window) ? p : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + e], factor, -ls[e]));
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + e], factor, -ls[e]));
       }
     }
-    if (r + 32 < r1) {
+    if (r + kRows < r1) {
       put(buf ^ 1);
-      if (r + 64 < r1) fetch(r + 64);
+      if (r + 2 * kRows < r1) fetch();
     }
     __syncthreads();
   }

@@ -47,7 +47,7 @@ void launch_attend(const AttendArgs& a, int d, int, bool, int tile_rows, hipStre
     a.part_ml[0] = a.part_ml[rows - 1] = float2{1.f, 1.f};
   }
 }
-void launch_merge(const AttendArgs& a, int, int, int, bool, hipStream_t) { ++merges; CHECK(a.splits > 1 || a.workers); }
+void launch_merge(const AttendArgs& a, int, int, bool, hipStream_t) { ++merges; CHECK(a.splits > 1 || a.workers); }
 void launch_weights(const AttendArgs& a, int, int, bool, hipStream_t) {
   ++weighings;
   CHECK(a.lse && a.weights_in && a.weights_out);
