@@ -7,7 +7,8 @@
 //
 // Bound by memory: a token is read and written once.  A wave works on one token; a lane moves 16 channels of a head at a time (two
 // 16-byte loads): the two octets of a rotated pair range, or 16 neighbours.  A lane keeps the same channels in every head, so its
-// eight sines and cosines are formed once: lane i forms pair i's, they cross lanes through LDS.
+// eight sines and cosines are formed once: lane i forms pair i's, they cross lanes through LDS.  Where a token belongs takes three loads that
+// wait for one another, so the token's own rows (up to UNITS pieces a lane) are requested before them.
 #include "../../include/kvx.h"
 #include "paged_types.h"
 
@@ -20,8 +21,7 @@ constexpr int kWaves = 4;
 constexpr int kMaxPairs = 64;
 
 template <typename T>
-__device__ __forceinline__ void load8(const uint8_t* p, float (&x)[8]) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ void floats(const u32x4& w, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = T::low(w[i]);
@@ -49,7 +49,7 @@ __device__ __forceinline__ void store8_e4m3(uint8_t* p, const float (&x)[8], flo
   *reinterpret_cast<u32x2*>(p) = w;
 }
 
-template <typename T, bool E4M3, bool INTERLEAVED>
+template <typename T, bool E4M3, bool INTERLEAVED, int UNITS>
 __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a, const int d, const int slabs) {
   __shared__ float2 trig[kWaves][kMaxPairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -57,6 +57,30 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
   const int64_t job = (int64_t)blockIdx.x * kWaves + wave;
   const int t = (int)(job / slabs), slab = (int)(job - (int64_t)t * slabs);
   if (t >= c.n_tokens) return;                       // whole waves leave; nothing below waits for another wave
+
+  // units of 16 channels: a head has d / 16; a multiple of them fits 64, so a lane's unit within its head is always the same
+  const int pairs = a.rotary >> 1, per_head = d >> 4, u = lane & (per_head - 1);
+  // The unit's two octets, so that neighbouring lanes have neighbouring octets: interleaved, octet u of each half of the head, pairs 4 c / 8 ..
+  // of both; half layout, the octets of pairs 8 u .. 8 u + 7, or octet u of each half of the channels that pass.
+  const int whole = a.rotary >> 4;                   // (half layout) units that turn
+  const bool turned = INTERLEAVED ? 8 * u < a.rotary : u < whole;
+  const int c0 = INTERLEAVED || turned ? 8 * u : a.rotary + 8 * (u - whole);
+  const int c1 = INTERLEAVED ? c0 + 8 * per_head : turned ? c0 + pairs : c0 + 8 * (per_head - whole);
+  const bool turned1 = INTERLEAVED ? c1 < a.rotary : turned;
+  const int hq = a.q.p ? c.hq : 0, heads = hq + 2 * c.hkv, heads_at_once = 64 / per_head;
+  const int h0 = heads_at_once * UNITS * slab + lane / per_head;
+  u32x4 raw[UNITS][2];
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    const int h = h0 + i * heads_at_once;
+    if (h >= heads) break;
+    const bool is_q = h < hq, is_v = h >= hq + c.hkv;
+    const Rows& from = is_q ? a.q : (is_v ? a.v : a.k);
+    const uint8_t* src = from.p + (int64_t)t * from.tok + (int64_t)(is_q ? h : is_v ? h - hq - c.hkv : h - hq) * from.head;
+    raw[i][0] = *reinterpret_cast<const u32x4*>(src + 2 * c0);
+    raw[i][1] = *reinterpret_cast<const u32x4*>(src + 2 * c1);
+  }
+
   const int b = sequence_of_row(c, t);
   if (b < 0) return;
   const Seq s = sequence(c, b);
@@ -68,7 +92,6 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
   const int slot = place & ((1 << c.page_shift) - 1);
   if (page < 0 && lane == 0) atomicOr(c.status, place < 0 ? kStatusLength : kStatusPage);
 
-  const int pairs = a.rotary >> 1;
   if (lane < pairs) {
     const int position = a.positions ? a.positions[t] : token;
     const uint64_t phase = (uint64_t)(int64_t)position * a.turns[lane];
@@ -79,44 +102,32 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                // the table crosses lanes of this wave only
   __builtin_amdgcn_wave_barrier();
 
-  // units of 16 channels: a head has d / 16; a multiple of them fits 64, so a lane's unit within its head is always the same
-  const int per_head = d >> 4;
-  const int u = lane & (per_head - 1);
-  const bool turned = u < (a.rotary >> 4);
-  int c0, c1, p0;                                                       // the unit's octets and its first pair
-  if (INTERLEAVED || !turned) {
-    c0 = 16 * u;
-    c1 = 16 * u + 8;
-  } else {
-    c0 = 8 * u;
-    c1 = 8 * u + pairs;
-  }
-  p0 = 8 * u;
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float2 w = trig[wave][turned ? p0 + i : 0];
+    const float2 w = trig[wave][INTERLEAVED ? (i < 4 ? (turned ? (c0 >> 1) + i : 0) : (turned1 ? (c1 >> 1) + i - 4 : 0)) : (turned ? 8 * u + i : 0)];
     cs[i] = w.x;
     sn[i] = w.y;
   }
-  const int hq = a.q.p ? c.hq : 0, heads = hq + 2 * c.hkv;
-  const int heads_at_once = 64 / per_head * slabs;
-  for (int h = 64 / per_head * slab + lane / per_head; h < heads; h += heads_at_once) {
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    const int h = h0 + i * heads_at_once;
+    if (h >= heads) break;
     const bool is_q = h < hq, is_v = h >= hq + c.hkv;
     const int kv = is_q ? 0 : (is_v ? h - hq - c.hkv : h - hq);
-    const Rows& from = is_q ? a.q : (is_v ? a.v : a.k);
-    const uint8_t* src = from.p + (int64_t)t * from.tok + (int64_t)(is_q ? h : kv) * from.head;
     float x0[8], x1[8];
-    load8<T>(src + 2 * c0, x0);
-    load8<T>(src + 2 * c1, x1);
+    floats<T>(raw[i][0], x0);
+    floats<T>(raw[i][1], x1);
     if (turned && !is_v) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float& lo = INTERLEAVED ? (i < 4 ? x0[2 * i] : x1[2 * i - 8]) : x0[i];
-        float& hi = INTERLEAVED ? (i < 4 ? x0[2 * i + 1] : x1[2 * i - 7]) : x1[i];
-        const float y0 = lo * cs[i] - hi * sn[i], y1 = hi * cs[i] + lo * sn[i];
-        lo = y0;
-        hi = y1;
+      for (int e = 0; e < 8; ++e) {
+        float& lo = INTERLEAVED ? (e < 4 ? x0[2 * e] : x1[2 * e - 8]) : x0[e];
+        float& hi = INTERLEAVED ? (e < 4 ? x0[2 * e + 1] : x1[2 * e - 7]) : x1[e];
+        const float y0 = lo * cs[e] - hi * sn[e], y1 = hi * cs[e] + lo * sn[e];
+        if (!INTERLEAVED || e < 4 || turned1) {
+          lo = y0;
+          hi = y1;
+        }
       }
     }
     if (is_q) {
@@ -146,12 +157,18 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
 }  // namespace
 
 void launch_append(const AppendArgs& a, int d, int dtype, bool e4m3, bool interleaved, hipStream_t st) {
-  const int heads = (a.q.p ? a.c.hq : 0) + 2 * a.c.hkv;
-  const int slabs = (heads * (d >> 4) + 63) / 64;
-  const int64_t jobs = (int64_t)a.c.n_tokens * slabs;
-  const dim3 grid((unsigned)((jobs + kWaves - 1) / kWaves)), block(64 * kWaves);
+  const int heads = (a.q.p ? a.c.hq : 0) + 2 * a.c.hkv, turns = (heads * (d >> 4) + 63) / 64;      // of 64 lanes, for a token
   auto go = [&](auto t, auto f8, auto inter) {
-    append_kernel<decltype(t), decltype(f8)::value, decltype(inter)::value><<<grid, block, 0, st>>>(a, d, slabs);
+    // four turns a wave where that leaves 8 waves a SIMD on 256 units, one for fewer tokens
+    auto with = [&](auto units) {
+      constexpr int kUnits = decltype(units)::value;
+      const int slabs = (turns + kUnits - 1) / kUnits;
+      const int64_t jobs = (int64_t)a.c.n_tokens * slabs;
+      append_kernel<decltype(t), decltype(f8)::value, decltype(inter)::value, kUnits>
+          <<<dim3((unsigned)((jobs + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, st>>>(a, d, slabs);
+    };
+    if ((int64_t)a.c.n_tokens * ((turns + 3) / 4) >= 8192) with(std::integral_constant<int, 4>{});
+    else with(std::integral_constant<int, 1>{});
   };
   auto by_layout = [&](auto t, auto f8) {
     if (interleaved) go(t, f8, std::true_type{});
