@@ -89,6 +89,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     // keys [all_lo, all_hi) are seen by every row
     const int all_hi = a.causal ? min(s.len, s.len - s.n + 1) : s.len;
     const int all_lo = a.window > 0 ? s.len - a.window : 0;
+    auto mixed = [&](int u, uint64_t absent) { return u + 32 > all_hi || u < all_lo || absent != 0; };
     const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
 
     const uint8_t* const kp = c.k + head_offset(c, head) + 16 * ld_chunk;
@@ -112,6 +113,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     float* const logits = a.logits && my_row < n_rows
                               ? a.logits + (((int64_t)b * c.hkv + head) * a.part_rows + my_row) * a.logit_stride + 4 * j : nullptr;
 
+    bool odd = false;
     int u = k0 + 32 * wave;
     if (u < k1) {
       fetch_page(u);
@@ -121,11 +123,14 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     for (; u < k1; u += 128) {
       const uint32_t absent = absent_next;
       // values behind the end and without a page are zero: a probability of zero times what lies there would not be
-      const bool tail = u + 32 > s.len || absent;
+      const bool some = mixed(u, absent);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int r = ld_row + i;
-        if (tail && (u + r >= s.len || ((absent >> r) & 1))) rv[i] = (u32x4){0, 0, 0, 0};
+        if (some) {
+          if (u + r >= s.len || ((absent >> r) & 1)) rv[i] = (u32x4){0, 0, 0, 0};
+          odd |= clean<T, E4M3>(rv[i]);
+        }
         *reinterpret_cast<u32x4*>(lk + lds_offset<kRB>(r, ld_chunk)) = rk[i];
         *reinterpret_cast<u32x4*>(lv + lds_offset<kRB>(r, ld_chunk)) = rv[i];
       }
@@ -137,7 +142,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
       }
       float x[W::kLogits];
       w.logits(lk, lane, x);
-      if (u + 32 > all_hi || u < all_lo || absent) w.mask(x, u, absent, j);
+      if (mixed(u, absent)) w.mask(x, u, absent, j);
       if (logits)
 #pragma unroll
         for (int g = 0; g < W::kLogits / 4; ++g)
@@ -163,6 +168,10 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
       for (int i = 0; i < W::kQuads; ++i)
         *reinterpret_cast<float4*>(jo + ((W::kSpan * i + 4 * j) ^ (4 * (my_row & 7)))) =
             make_float4(w.quad(i, 0) * mine, w.quad(i, 1) * mine, w.quad(i, 2) * mine, w.quad(i, 3) * mine);
+    if (__ballot(odd))
+      mend_odd_values<T, D, E4M3, 32>(c, b, head, s.len, k0 + 32 * wave, k1, 128, mixed, w.lo, w.hi, W::kSpan, j, [&](int i, int e, float x) {
+        if (my_row < n_rows) jo[(W::kSpan * i + 4 * j + e) ^ (4 * (my_row & 7))] += x;
+      });
     __syncthreads();
     const float v_scale = E4M3 && c.v_scale ? c.v_scale[head] : 1.f;
     const int64_t part = ((int64_t)blockIdx.x * 2 + (unit == col.first ? 1 : 0)) * a.part_rows;
@@ -273,11 +282,17 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lds + buf * kTile + lds_offset<kRB>(ld_row + i, ld_chunk)) = r[i];
   };
+  const int block_hi = uniform(a.causal ? min(s.len, s.len - s.n + row0 / c.group + 1) : s.len);
+  const int block_lo = uniform(a.window > 0 ? s.len - s.n + (row0 + n_rows - 1) / c.group + 1 - a.window : 0);
+  auto mixed = [&](int u, uint64_t missing) { return u + 64 > block_hi || u < block_lo || missing != 0; };
+  bool odd = false;
   auto put_v = [&](int buf, int u) {                         // values behind the end and without a page are zero
-    if (u + 64 > s.len || absent_loaded)
+    if (mixed(u, absent_loaded))
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
+      for (int i = 0; i < kLoads; ++i) {
         if (u + ld_row + i >= s.len || ((absent_loaded >> (ld_row + i)) & 1)) rv[i] = (u32x4){0, 0, 0, 0};
+        odd |= clean<T, E4M3>(rv[i]);
+      }
     put(rv, 3 + buf);
   };
   auto live = [&](int key0) { return key0 < k1 && key0 < any_hi && key0 + 32 > any_lo; };
@@ -359,24 +374,43 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
     const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
     w.l = __uint_as_float(z[0]) + __uint_as_float(z[1]);
   }
-  if (first + (lane & 31) > last) return;
+  const bool mine = first + (lane & 31) <= last;
   const int token = s.first + i_row, qh = head * c.group + g_row;
   const bool whole = n_splits == 1;
   const int64_t part_row = (((int64_t)tile * c.hkv + head) * a.splits + split) * a.part_rows + (row - row0);
   const float f = whole ? (w.l == 0.f ? 0.f : (E4M3 && c.v_scale ? c.v_scale[head] : 1.f) / w.l) : 1.f;
+  if (mine) {
 #pragma unroll
-  for (int cb = 0; cb < S::kBlocks; ++cb)
+    for (int cb = 0; cb < S::kBlocks; ++cb)
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int ch = 32 * cb + 8 * g + 4 * h;
-      const float o[4] = {w.o[cb][4 * g] * f, w.o[cb][4 * g + 1] * f, w.o[cb][4 * g + 2] * f, w.o[cb][4 * g + 3] * f};
-      if (whole) store_out<T>(a, token, qh, ch, o);
-      else *reinterpret_cast<float4*>(a.part_o + part_row * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
+      for (int g = 0; g < 4; ++g) {
+        const int ch = 32 * cb + 8 * g + 4 * h;
+        const float o[4] = {w.o[cb][4 * g] * f, w.o[cb][4 * g + 1] * f, w.o[cb][4 * g + 2] * f, w.o[cb][4 * g + 3] * f};
+        if (whole) store_out<T>(a, token, qh, ch, o);
+        else *reinterpret_cast<float4*>(a.part_o + part_row * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
+      }
+    if (h == 0) {
+      if (!whole) a.part_ml[part_row] = make_float2(w.m, w.l);
+      else if (a.lse) a.lse[(int64_t)token * c.hq + qh] = log_sum(w.m, w.l);
     }
-  if (h == 0) {
-    if (!whole) a.part_ml[part_row] = make_float2(w.m, w.l);
-    else if (a.lse) a.lse[(int64_t)token * c.hq + qh] = log_sum(w.m, w.l);
   }
+  // whether any thread met one: a word of the tiles, which are read no more (the kernel has no LDS to spare: 80 KB a workgroup, two of them)
+  int* const any_odd = reinterpret_cast<int*>(lds);
+  if (threadIdx.x == 0) *any_odd = 0;
+  __syncthreads();
+  if (odd) *any_odd = 1;
+  __syncthreads();
+  if (*any_odd)                                              // (a lane adds to what it has just written)
+    mend_odd_values<T, D, E4M3, 64>(c, b, head, s.len, k0, k1, 64, mixed, w.lo, w.hi, 8, h, [&](int i, int e, float x) {
+      const int ch = 8 * i + 4 * h + e;
+      if (!mine) return;
+      if (whole) {
+        uint16_t* const at = reinterpret_cast<uint16_t*>(a.out.p + (int64_t)token * a.out.tok + (int64_t)qh * a.out.head) + ch;
+        *at = (uint16_t)T::pack(T::low(*at) + x, 0.f);
+      } else {
+        a.part_o[part_row * D + ch] += x;
+      }
+    });
 }
 
 // ---- partial results ------------------------------------------------------------------------------------------------

@@ -356,6 +356,56 @@ __device__ __forceinline__ int32_t page_of_key(const Call& c, int b, int key, in
 }
 __device__ __forceinline__ uint64_t row_offset(const Call& c, int32_t page, int key) { return slot_offset(c, page, key & ((1 << c.page_shift) - 1)); }
 
+// Keys that some rows of a workgroup or wave see and others do not ("mixed" runs of KEYS keys, see mixed() in the kernels): an infinite value
+// or NaN among theirs belongs to the rows that see its key, but a probability of zero times it is NaN in all of them.  So the values of
+// mixed runs come into LDS without such (clean tells whether there were any), and where there were, this adds them in the end to the
+// outputs of the rows that see them, where those lie in memory.  Rare; all lanes of a wave together.  A lane has one row, which sees keys
+// [lo, hi), and of its channels the quads span * q + 4 * part .. + 3; add(q, e, x) adds x to the e-th of quad q.
+template <typename T, bool E4M3>
+__device__ __forceinline__ bool clean(u32x4& r) {
+  bool odd = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t w = finite_part<T, E4M3>(r[e]);
+    odd |= w != r[e];
+    r[e] = w;
+  }
+  return odd;
+}
+template <typename T, int D, bool E4M3, int KEYS, typename MIXED, typename ADD>
+__device__ __forceinline__ void mend_odd_values(const Call& c, int b, int head, int len, int k0, int k1, int step, MIXED mixed, int lo, int hi, int span, int part,
+                                                ADD add) {
+  const int lane = threadIdx.x & 63;
+  for (int u = k0; u < k1; u += step) {
+    const int32_t page = page_of_key(c, b, u + lane % KEYS, len);
+    const uint64_t absent = __ballot(page < 0);
+    if (!mixed(u, absent)) continue;
+    for (int i = 0; i < KEYS && u + i < len; ++i) {
+      if ((absent >> i) & 1) continue;
+      const uint8_t* v = c.v + head_offset(c, head) + row_offset(c, __shfl(page, i), u + i);
+      const bool sees = u + i >= lo && u + i < hi;
+#pragma unroll 1
+      for (int q = 0; q * span < D; ++q) {
+        const int ch = q * span + 4 * part;
+        uint32_t w[2];
+        if constexpr (E4M3) {
+          const uint32_t x = *reinterpret_cast<const uint32_t*>(v + ch);
+          w[0] = T::template from_e4m3<false>(x);
+          w[1] = T::template from_e4m3<true>(x);
+        } else {
+          w[0] = *reinterpret_cast<const uint32_t*>(v + 2 * ch);
+          w[1] = *reinterpret_cast<const uint32_t*>(v + 2 * ch + 4);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = e & 1 ? T::high(w[e >> 1]) : T::low(w[e >> 1]);
+          if (sees && !(fabsf(x) < kInf)) add(q, e, x);
+        }
+      }
+    }
+  }
+}
+
 // Which rows a workgroup works on: row tile `t` of sequence `b`; false: none.
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, int tile, int tile_rows, int& b, int& t) {
   if (a.tiles_per_seq > 0) {

@@ -21,6 +21,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 struct Half {
+  static constexpr uint32_t kExponent = 0x7C00u;
   // two floats rounded to nearest even, the first in the low half
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
@@ -39,6 +40,7 @@ struct Half {
   }
 };
 struct Brain {
+  static constexpr uint32_t kExponent = 0x7F80u;
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
   }
@@ -54,6 +56,19 @@ struct Brain {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, UPPER));
   }
 };
+
+// A word without its infinities and NaN (two values of T, or four of 8 bits, which have no infinities).
+template <typename T, bool E4M3>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  if constexpr (E4M3) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) r |= ((w >> i) & 0x7Fu) == 0x7Fu ? 0u : w & (0xFFu << i);
+    return r;
+  } else {
+    return ((w & T::kExponent) == T::kExponent ? 0u : w & 0xFFFFu) | (((w >> 16) & T::kExponent) == T::kExponent ? 0u : w & 0xFFFF0000u);
+  }
+}
 
 // Eight 8-bit floats as eight values of T, in order.
 template <typename T>

@@ -189,3 +189,44 @@ def test_the_same_call_twice_gives_the_same_bits(new):
         h.attend(case.pages(), case.batch(), q, o, weights_out=w)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and torch.equal(ws[0], ws[1]) and torch.equal(ws[0], ws[2])
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 4, 9, 100])
+@pytest.mark.parametrize("window", [0, 30])
+def test_what_a_row_does_not_see_has_no_part_in_it(dtype, cache, d, new, window):
+    """Infinities and NaN in keys and values: rows that do not see them are what they would be without, rows that see an infinite value have it."""
+    case = pu.Case([150], [new], hq=4, hkv=2, d=d, page=16, dtype=dtype, cache=cache, seed=new + d)
+    last = 150 - new
+    odd = {last + new // 2: float("nan"), last + new - 1: float("inf")} if new > 1 else {}
+    if window:
+        odd.update({last - window - 3: float("nan"), last - window: -float("inf")})
+    if new > 20:
+        odd[last + 17] = -float("inf")
+    for j, x in odd.items():
+        page, slot = po.place(case.pool, 0, j)
+        x = x if cache != "e4m3" else float("nan")
+        case.pool["v"][page, slot, :, 5:9] = x
+        v = torch.full((2, 4), x).to(pu.TYPES[cache])
+        case.v.view(torch.uint8 if cache == "e4m3" else torch.int16)[page, slot, :, 5:9] = v.view(torch.uint8 if cache == "e4m3" else torch.int16).to(case.device)
+    hidden = [j for j in odd if window and j <= last - window]       # seen by no row: their keys too
+    for j in hidden:
+        page, slot = po.place(case.pool, 0, j)
+        case.pool["k"][page, slot] = float("nan")
+        nan = torch.full((2, d), float("nan")).to(pu.TYPES[cache])
+        case.k.view(torch.uint8 if cache == "e4m3" else torch.int16)[page, slot] = nan.view(torch.uint8 if cache == "e4m3" else torch.int16).to(case.device)
+    h, q = case.handle(), case.rows(4)
+    out = torch.empty_like(q)
+    lse = torch.empty(case.n_tokens, 4, device=case.device)
+    w_out = torch.zeros_like(case.weights)
+    h.attend(case.pages(), case.batch(), q, out, lse=lse, window=window, weights_out=w_out)
+    torch.cuda.synchronize()
+    scales = [None if x is None else x.numpy() for x in (case.k_scale, case.v_scale)]
+    with np.errstate(invalid="ignore"):
+        ref, rl, gained, absolute, reach = po.attend(case.pool, q.float().cpu().numpy(), case.start, case.lens, 1 / math.sqrt(d), True, window, *scales)
+    finite = np.where(np.isfinite(absolute), absolute, 0.0)
+    b_out, b_lse, b_w = pu.attend_bounds(case, np.where(np.isfinite(ref), ref, 0.0), finite, rl, gained, reach, new * 2 <= 32)
+    pu.check(out.float().cpu().numpy(), ref, b_out, "out")
+    pu.check(lse.cpu().numpy(), rl, b_lse, "lse")
+    pu.check(w_out.cpu().numpy(), gained, b_w, "weights")
