@@ -256,31 +256,38 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   const int all_lo = uniform(a.window > 0 ? place_last + 1 - a.window : 0), any_lo = uniform(a.window > 0 ? place_first + 1 - a.window : 0);
   const float factor = a.factor * (E4M3 && c.k_scale ? c.k_scale[head] : 1.f);
 
-  // A wave brings 16 neighbouring rows, which lie in one or two pages: their places are scalars but for the lane's own part.
+  // A wave brings 16 neighbouring rows: eight of them and eight, whose places are scalars but for the lane's own part.
   const int ld_row = threadIdx.x / kLPR * kLoads, ld_chunk = threadIdx.x % kLPR, slot_mask = (1 << c.page_shift) - 1;
-  const uint64_t slot_bytes = (uint64_t)c.slot_stride << 4, lane_part = (uint64_t)(ld_row & slot_mask) * slot_bytes + 16 * ld_chunk;
+  const uint64_t slot_bytes = (uint64_t)c.slot_stride << 4, lane_part = (uint64_t)(ld_row & 7) * slot_bytes + 16 * ld_chunk;
   const uint8_t* const kp = c.k + head_offset(c, head);
   const uint8_t* const vp = c.v + head_offset(c, head);
   u32x4 rk[kLoads], rv[kLoads];                              // rows on their way
-  int32_t page_k = 0, page_v = 0;                            // of a tile's keys, one a lane: the tiles of K and of V whose rows are loaded next
-  uint64_t absent_loaded = 0;                                // keys without a page: of the tile of V in the registers
+  // Where a tile's rows lie, a key a lane: of the tiles of K and of V whose rows are loaded next, with the keys that have no page.
+  struct Tile {
+    uint64_t at, absent;
+  };
+  Tile tile_k{0, 0}, tile_v{0, 0};
+  uint64_t absent_loaded = 0;                                // of the tile of V in the registers
+  int32_t page = 0;                                          // of the tile after tile_k
   auto page_at = [&](int u) { return u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
-  auto fetch = [&](u32x4 (&r)[kLoads], const uint8_t* p, int32_t page, int u) {
-    const int first_row = 16 * wave;                         // (u is a multiple of 64: u & slot_mask is 0 in pages of fewer slots)
-    const uint64_t low = slot_offset(c, __builtin_amdgcn_readlane(page, first_row), u & slot_mask);
-    const uint64_t high = slot_offset(c, __builtin_amdgcn_readlane(page, first_row + 8), u & slot_mask);
-    const uint8_t* const q = p + (ld_row - first_row < 8 ? low : high) + lane_part;
+  auto tile_at = [&](int32_t pg, int u) { return Tile{slot_offset(c, pg, (u + (lane & 56)) & slot_mask), __ballot(pg < 0)}; };      // (eight rows share it)
+  auto fetch = [&](u32x4 (&r)[kLoads], const uint8_t* p, const Tile& t) {
+    auto of_row = [&](int row) {
+      return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t.at, row) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(t.at >> 32), row) << 32;
+    };
+    const uint64_t low = of_row(16 * wave), high = of_row(16 * wave + 8);
+    const uint8_t* const q = p + (ld_row - 16 * wave < 8 ? low : high) + lane_part;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) r[i] = *reinterpret_cast<const u32x4*>(q + i * slot_bytes);
   };
-  auto fetch_v = [&](int u) {
-    absent_loaded = __ballot(page_v < 0);
+  auto fetch_v = [&]() {
+    absent_loaded = tile_v.absent;
     if (absent_loaded && threadIdx.x == 0) note_bad_page(c);
-    fetch(rv, vp, page_v, u);
+    fetch(rv, vp, tile_v);
   };
   auto put = [&](const u32x4 (&r)[kLoads], int buf) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lds + buf * kTile + lds_offset<kRB>(ld_row + i, ld_chunk)) = r[i];
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4*>(lds + buf + lds_offset<kRB>(ld_row + i, ld_chunk)) = r[i];
   };
   const int block_hi = uniform(a.causal ? min(s.len, s.len - s.n + row0 / c.group + 1) : s.len);
   const int block_lo = uniform(a.window > 0 ? s.len - s.n + (row0 + n_rows - 1) / c.group + 1 - a.window : 0);
@@ -293,47 +300,52 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
         if (u + ld_row + i >= s.len || ((absent_loaded >> (ld_row + i)) & 1)) rv[i] = (u32x4){0, 0, 0, 0};
         odd |= clean<T, E4M3>(rv[i]);
       }
-    put(rv, 3 + buf);
+    put(rv, buf);
   };
-  auto live = [&](int key0) { return key0 < k1 && key0 < any_hi && key0 + 32 > any_lo; };
+  // units [live_from, + live_keys) hold a key that one of the wave's rows sees, units [clear_from, + clear_keys) only keys that all of them see: one
+  // comparison each, for scalar instructions count too (a unit took 69 of them, 124 vector ones and 8 matrix ones at d = 64)
+  const int live_from = any_lo - 31, clear_from = all_lo;
+  const uint32_t live_keys = (uint32_t)max(0, min(k1, any_hi) - live_from), clear_keys = (uint32_t)max(0, all_hi - 31 - all_lo);
+  auto live = [&](int key0) { return (uint32_t)(key0 - live_from) < live_keys; };
 
   // in LDS before the first tile: its K and V and the next one's K; on the way: the next one's V and the third one's K
   uint64_t absent = 0;                                       // of the running tile
   f32x16 x, y;                                               // logits of the running unit, then its probabilities; of the next one
   if (k0 < k1) {
-    page_v = page_at(k0);
-    fetch(rk, kp, page_v, k0);
-    fetch_v(k0);
-    page_k = page_at(k0 + 64);
+    tile_v = tile_at(page_at(k0), k0);
+    fetch(rk, kp, tile_v);
+    fetch_v();
+    tile_k = tile_at(page_at(k0 + 64), k0 + 64);
     put(rk, 0);
-    put_v(0, k0);
+    put_v(3 * kTile, k0);
     absent = absent_loaded;
     if (k0 + 64 < k1) {
-      fetch(rk, kp, page_k, k0 + 64);
-      page_v = page_k;
-      fetch_v(k0 + 64);
-      page_v = page_at(k0 + 128);
-      put(rk, 1);
-      if (k0 + 128 < k1) fetch(rk, kp, page_v, k0 + 128);
-      page_k = page_at(k0 + 192);
+      fetch(rk, kp, tile_k);
+      tile_v = tile_k;
+      fetch_v();
+      tile_v = tile_at(page_at(k0 + 128), k0 + 128);
+      put(rk, kTile);
+      if (k0 + 128 < k1) fetch(rk, kp, tile_v);
+      tile_k = tile_at(page_at(k0 + 192), k0 + 192);
+      page = page_at(k0 + 256);
     }
   }
   __syncthreads();
-  int kb = 0, vb = 0;                                        // buffers of the running tile
-  if (live(k0)) x = w.logits(lds, lane);
+  int kb = 0, kb1 = kTile, kb2 = 2 * kTile, vb = 3 * kTile, vb1 = 4 * kTile;      // buffers: K of the running tile and the next two, V of it and the next
+  bool now = live(k0);
+  if (now) x = w.logits(lds, lane);
   for (int u = k0; u < k1; u += 64) {
-    const int kb1 = kb == 2 ? 0 : kb + 1, kb2 = kb1 == 2 ? 0 : kb1 + 1;
     uint64_t absent_next = 0;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int key0 = u + 32 * half;
-      const uint8_t* const k_now = lds + kb * kTile + half * 32 * kRB;
-      const uint8_t* const k_next = half == 0 ? lds + kb * kTile + 32 * kRB : lds + kb1 * kTile;
-      const uint8_t* const v_now = lds + (3 + vb) * kTile + half * 32 * kRB;
-      const bool now = live(key0), next = live(key0 + 32);
+      const uint8_t* const k_now = lds + kb + half * 32 * kRB;
+      const uint8_t* const k_next = half == 0 ? lds + kb + 32 * kRB : lds + kb1;
+      const uint8_t* const v_now = lds + vb + half * 32 * kRB;
+      const bool next = live(key0 + 32);
       if (now) {
         const uint32_t missing = (uint32_t)(absent >> (32 * half));
-        const bool masked = key0 + 32 > all_hi || key0 < all_lo || missing;
+        const bool masked = (uint32_t)(key0 - clear_from) >= clear_keys || missing;
         if (masked) w.mask(x, key0, missing, h);
         float sum = next ? w.template soften<true>(x, factor, k_next, lane, y) : w.template soften<false>(x, factor, k_next, lane, y);
         if (__ballot(sum > kMost || w.m == -kInf)) {         // rare: form the unit again and raise m to its largest
@@ -350,23 +362,29 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
         y = w.logits(k_next, lane);
       }
       x = y;
+      now = next;
       // into buffers that were read last in the tile before this one, a barrier ago
       if (half == 0) {
         if (u + 64 < k1) {
-          put_v(vb ^ 1, u + 64);
+          put_v(vb1, u + 64);
           absent_next = absent_loaded;
         }
-        if (u + 128 < k1) fetch_v(u + 128);
+        if (u + 128 < k1) fetch_v();
       } else if (u + 128 < k1) {
         put(rk, kb2);
-        if (u + 192 < k1) fetch(rk, kp, page_k, u + 192);
-        page_v = page_k;
-        page_k = page_at(u + 256);
+        if (u + 192 < k1) fetch(rk, kp, tile_k);
+        tile_v = tile_k;
+        tile_k = tile_at(page, u + 256);
+        page = page_at(u + 320);
       }
     }
     __syncthreads();
+    const int kb_free = kb, vb_free = vb;
     kb = kb1;
-    vb ^= 1;
+    kb1 = kb2;
+    kb2 = kb_free;
+    vb = vb1;
+    vb1 = vb_free;
     absent = absent_next;
   }
 
