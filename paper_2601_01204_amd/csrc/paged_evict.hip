@@ -3,7 +3,7 @@
 // select_kernel, one workgroup per (sequence, key head).  Weights become 32-bit keys in the same order (NaN below -infinity, tokens
 // whose page is missing below that; protected tokens above everything), and the budget-th largest key is found digit by digit
 // (11, 11 and 10 bits: 11 bits take sign, exponent and two bits of the mantissa, so that weights of a few orders of magnitude spread over
-// dozens of counters).  Among equal keys the lower slots stay.  Then every wave walks a contiguous part of the slots: slots below the
+// dozens of counters).  Where a few tokens leave (decoding: one), they are found as the least keys instead.  Among equal keys the lower slots stay.  Then every wave walks a contiguous part of the slots: slots below the
 // budget that lose their token and tokens behind it that stay are numbered in ascending order by ballots, and the i-th of the
 // ones receives the i-th of the others.  Sources lie behind the budget and destinations before it, so the moves are free of
 // order.
@@ -22,6 +22,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
 constexpr int kFewMoves = 256;
+constexpr int kFewLeave = 4;                    // tokens that leave by looking for the least: a pass each, where the digits take three longer ones
 
 __device__ __forceinline__ uint32_t key_of(const EvictArgs& a, int32_t id, float w, int seen) {
   if (id < a.sinks || id >= seen - a.recent) return kProtected;
@@ -42,7 +43,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, int b, int head, c
     if (from < 0 || to < 0) continue;                                // (a token without a page never stays unless the budget asks for it)
     const uint64_t src = slot_offset(c, from, m.x & mask) + head_offset(c, head) + 16 * chunk;
     const uint64_t dst = slot_offset(c, to, m.y & mask) + head_offset(c, head) + 16 * chunk;
-    const u32x4 k = *reinterpret_cast<const u32x4*>(c.k + src), v = *reinterpret_cast<const u32x4*>(c.v + src);
+    const u32x4 k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(c.k + src)), v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(c.v + src));
     *reinterpret_cast<u32x4*>(c.k + dst) = k;
     *reinterpret_cast<u32x4*>(c.v + dst) = v;
     if (chunk == 0) {
@@ -95,8 +96,9 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, con
   const int len = s.len, budget = a.budget, seen = c.seen[b], mask = (1 << c.page_shift) - 1;
   const bool over = len > budget, in_place = a.weights_out == c.weights && a.ids_out == c.ids;
   int2* const moves = a.moves + (int64_t)blockIdx.x * a.max_moves;
-  // a wave has a contiguous part of the slots, 256 at a time
-  const int its = (len + 4 * kThreads - 1) / (4 * kThreads), part = its * 256, j0 = min(len, wave * part), j1 = min(len, j0 + part);
+  // a wave has a contiguous part of the slots, 256 at a time (short caches: of all that the launch provides for, so that the page table can be
+  // read before the length is there)
+  const int its = NIT == 1 || NIT == 2 ? NIT : (len + 4 * kThreads - 1) / (4 * kThreads), part = its * 256, j0 = wave * part, j1 = min(len, j0 + part);
 
   struct Group {
     int32_t page;
@@ -105,11 +107,11 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, con
   };
   auto slot_of = [&](int it) { return j0 + 256 * it + 4 * lane; };
   auto index_of = [&](int32_t page, int j) { return (((int64_t)page * c.hkv + head) << c.page_shift) + (j & mask); };
-  auto load_page = [&](Group& g, int it) { g.page = slot_of(it) < j1 ? page_of(c, b, slot_of(it) >> c.page_shift) : -1; };
+  auto load_page = [&](Group& g, int it) { g.page = slot_of(it) < c.max_len ? page_of(c, b, slot_of(it) >> c.page_shift) : -1; };
   auto load_rest = [&](Group& g, int it) {
     int4 i4 = make_int4(0, 0, 0, 0);
     float4 w4 = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (g.page >= 0) {
+    if (g.page >= 0 && slot_of(it) < j1) {
       const int64_t at = index_of(g.page, slot_of(it));
       i4 = *reinterpret_cast<const int4*>(c.ids + at);
       w4 = *reinterpret_cast<const float4*>(c.weights + at);
@@ -233,9 +235,50 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, con
     return;
   }
 
-  // the budget-th largest key, and how many of those equal to it stay
+  // the key at which the staying ones end, and how many of those equal to it stay
   uint32_t prefix = 0;
   int want = budget;
+  if (len - budget <= kFewLeave) {
+    // few leave: the least keys one after the other, each with its count
+    uint32_t least = 0;                         // keys below it have been counted
+    for (int leave = len - budget;;) {
+      uint32_t low = kProtected;
+      int count = 0;
+      each([&](int, int j, const uint32_t (&k)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < j1 && k[e] >= least) {
+            count = k[e] < low ? 1 : count + (k[e] == low);
+            low = min(low, k[e]);
+          }
+      });
+      auto join = [&](uint32_t l, int n) {
+        count = l < low ? n : count + (l == low ? n : 0);
+        low = min(low, l);
+      };
+#pragma unroll
+      for (int o = 32; o; o >>= 1) join((uint32_t)__shfl_xor((int)low, o), __shfl_xor(count, o));
+      __syncthreads();                          // the last use of sums is over
+      if (lane == 0) sums[wave] = make_int2((int)low, count);
+      __syncthreads();
+      low = kProtected;
+      count = 0;
+      int2 all[kWaves];
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) all[i] = sums[i];
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) join((uint32_t)all[i].x, all[i].y);
+      if (count >= leave || low == kProtected) {
+        prefix = low;
+        want = max(0, count - leave);
+        if (threadIdx.x == 0) found[2] = count;
+        break;
+      }
+      leave -= count;
+      least = low + 1;
+    }
+    __syncthreads();
+  } else {
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
@@ -271,6 +314,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const EvictArgs a, con
     __syncthreads();
     prefix |= (uint32_t)found[0] << shift;
     want = found[1];                            // (read before the next pass's first barrier, written behind its second)
+  }
   }
   const bool ranked = want < found[2];          // not all of the equal ones stay
 
@@ -381,7 +425,7 @@ void launch_evict(const EvictArgs& a, int d, bool e4m3, int32_t* arrived, hipStr
     else select_kernel<kRB, 0><<<grid, block, 0, st>>>(a, here, arrived);
     if (!here) {
       const int rows = 256 / (kRB / 16);
-      int parts = (a.max_moves + 4 * rows - 1) / (4 * rows);          // four rows a lane group where every move happens
+      int parts = (a.max_moves + 2 * rows - 1) / (2 * rows);          // two rows a lane group where every move happens
       if ((int64_t)parts * jobs > (1 << 20)) parts = (1 << 20) / jobs > 0 ? (1 << 20) / jobs : 1;
       move_kernel<kRB><<<dim3((unsigned)(parts * jobs)), dim3(256), 0, st>>>(a, parts);
     }
