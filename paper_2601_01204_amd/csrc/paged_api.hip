@@ -252,6 +252,17 @@ void plan_splits(const kv_paged* h, AttendArgs& a) {
   a.splits = (int32_t)splits;
 }
 
+// Parts of the rows in the launch that forms weights again: as many as give a compute unit four workgroups, of at least 256 rows.  Their sums lie
+// where attention's partial results were, which the merge in front of it has read.
+void plan_weights(const kv_paged* h, AttendArgs& a) {
+  const int64_t stride = align_up(a.c.max_len, 128), blocks = stride / 128 * a.c.hkv * a.c.n_seqs;
+  const int64_t rows = (int64_t)a.c.max_new * h->group, fit = h->part_rows_cap * h->cfg.head_dim / (128 * blocks);
+  const int64_t splits = std::min(std::min<int64_t>(4ll * h->n_cus / blocks, rows / 256), std::min<int64_t>(fit, 32));
+  a.weight_splits = (int32_t)std::max<int64_t>(1, splits);
+  a.weight_stride = (int32_t)stride;
+  a.weight_part = (float*)h->work;
+}
+
 }  // namespace
 
 extern "C" {
@@ -368,6 +379,8 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   if (weights_out && !a.c.weights) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out needs pages->weights");
   if ((uintptr_t)lse & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse must be 4-byte aligned");
   if ((uintptr_t)weights_out & 15) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out must be 16-byte aligned");
+  // units of 128 keys of all sequences and key heads are counted in 32 bits, and are the workgroups that form weights again
+  if ((int64_t)a.c.n_seqs * ((a.c.max_len + 127) / 128) * a.c.hkv > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: n_seqs * max_len * n_kv_heads is too large");
   hipStream_t st = (hipStream_t)hip_stream;
   const kv_paged_config& c = h->cfg;
   const bool e4m3 = c.cache_dtype == KV_E4M3;
@@ -395,7 +408,10 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
     if (a.splits > 1 || a.workers) launch_merge(a, c.head_dim, c.dtype, e4m3, st);
   }
   if (a.logits) launch_weights_from_logits(a, st);
-  else if (weights_out) launch_weights(a, c.head_dim, c.dtype, e4m3, st);
+  if (weights_out && !a.logits) {
+    plan_weights(h, a);
+    launch_weights(a, c.head_dim, c.dtype, e4m3, st);
+  }
   return launched(h, "kv_paged_attend");
 }
 

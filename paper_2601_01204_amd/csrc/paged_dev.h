@@ -50,6 +50,8 @@ struct AttendArgs {
   float2* part_ml;
   const float* weights_in;
   float* weights_out;
+  float* weight_part;           // [weight_splits][sequence][key head][weight_stride] sums over parts of the rows, where there is more than one
+  int32_t weight_splits, weight_stride;
   float* logits;                // launches of few rows that collect weights: [tile][key head][row][logit_stride], log2 units; NULL: not kept
   int64_t logit_stride;
   float factor;                 // softmax scale * log2(e)

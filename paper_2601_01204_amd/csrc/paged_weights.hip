@@ -7,7 +7,8 @@
 // weights_kernel.  A workgroup owns 128 keys of one key head, a wave 32 of them, whose fragments stay in registers, and goes over all rows that see
 // them, 64 at a time, brought into LDS for the four waves.  S = Q K^T with a key in a lane and its rows in that lane's registers: a key's
 // weights are summed in its lane, in row order, in fp32 without a rounding between, and no two workgroups write the same
-// token, so the sums do not depend on what ran when.
+// token, so the sums do not depend on what ran when.  Where there are too few workgroups for the chip the rows are cut into parts as well,
+// whose sums weights_sum_kernel adds in order (five sequences of 481 tokens, 410 of them new, 24 heads: XXX us).
 #include "../../include/kvx.h"
 #include "paged_tile.h"
 
@@ -30,7 +31,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int key_blocks = (c.max_len + kKeys - 1) / kKeys;
   const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
-  const int block = rest % key_blocks, b = rest / key_blocks;
+  const int block = rest % key_blocks, column = rest / key_blocks, b = column % c.n_seqs, split = column / c.n_seqs;
   const Seq s = uniform(sequence(c, b));
   const int kb = block * kKeys;
   if (kb >= s.len) return;
@@ -59,7 +60,8 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   const int base = s.len - s.n;
   const int i0 = a.causal ? min(s.n, max(0, kb - base)) : 0;
   const int i1 = a.window > 0 ? max(i0, min(s.n, kb + kKeys - 1 + a.window - base)) : s.n;
-  const int r0 = uniform(i0 * c.group), r1 = uniform(i1 * c.group);
+  const int rows = (i1 - i0) * c.group, part = (rows + a.weight_splits * kRows - 1) / (a.weight_splits * kRows) * kRows;
+  const int r0 = uniform(i0 * c.group + min(rows, split * part)), r1 = uniform(i0 * c.group + min(rows, (split + 1) * part));
   // A thread brings the same rows of every kRows: their tokens and heads move on by the same steps (a division by the group would cost more
   // than a row's exponentials).
   struct Place {
@@ -156,10 +158,28 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   }
   const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
   sum = __uint_as_float(w[0]) + __uint_as_float(w[1]);
-  if (h == 0 && page >= 0) {
+  if (a.weight_splits > 1) {
+    if (h == 0) a.weight_part[((int64_t)column * c.hkv + head) * a.weight_stride + key] = sum;
+  } else if (h == 0 && page >= 0) {
     const int64_t at = (((int64_t)page * c.hkv + head) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
     a.weights_out[at] = a.weights_in[at] + sum;
   }
+}
+
+// The sums over the parts of the rows, a key a thread.
+__global__ __launch_bounds__(256) void weights_sum_kernel(const AttendArgs a) {
+  const Call& c = a.c;
+  const int key_blocks = (c.max_len + 255) / 256;
+  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv, b = rest / key_blocks, key = (rest - b * key_blocks) * 256 + (int)threadIdx.x;
+  const Seq s = sequence(c, b);
+  if (key >= s.len) return;
+  const int32_t page = page_of(c, b, key >> c.page_shift);
+  if (page < 0) return;
+  float sum = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < a.weight_splits; ++i) sum += a.weight_part[(((int64_t)i * c.n_seqs + b) * c.hkv + head) * a.weight_stride + key];
+  const int64_t at = (((int64_t)page * c.hkv + head) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+  a.weights_out[at] = a.weights_in[at] + sum;
 }
 
 // A thread has four neighbouring keys of one key head.  A row's range of keys (row tiles of decoding see them all but for masks) was
@@ -222,7 +242,7 @@ void launch_weights_from_logits(const AttendArgs& a, hipStream_t st) {
 }
 
 void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)((a.c.max_len + kKeys - 1) / kKeys) * a.c.hkv * a.c.n_seqs));
+  const dim3 grid((unsigned)((int64_t)((a.c.max_len + kKeys - 1) / kKeys) * a.c.hkv * a.c.n_seqs * a.weight_splits));
   auto go = [&](auto t, auto dd, auto f8) { weights_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a); };
   auto by_d = [&](auto t, auto f8) {
     if (d == 128) go(t, std::integral_constant<int, 128>{}, f8);
@@ -234,6 +254,7 @@ void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_
   };
   if (dtype == KV_F16) by_cache(Half{});
   else by_cache(Brain{});
+  if (a.weight_splits > 1) weights_sum_kernel<<<dim3((unsigned)((int64_t)((a.c.max_len + 255) / 256) * a.c.hkv * a.c.n_seqs)), dim3(256), 0, st>>>(a);
 }
 
 }  // namespace paged

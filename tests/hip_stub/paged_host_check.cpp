@@ -23,7 +23,7 @@
 
 namespace kvx {
 namespace paged {
-static int64_t appends, attends, merges, weighings, evictions;
+static int64_t appends, attends, merges, weighings, weight_parts, evictions;
 static AttendArgs last;
 static AppendArgs last_append;
 static int last_rows;
@@ -52,6 +52,11 @@ void launch_weights(const AttendArgs& a, int, int, bool, hipStream_t) {
   ++weighings;
   CHECK(a.lse && a.weights_in && a.weights_out);
   if (a.c.n_tokens) a.lse[(int64_t)a.c.n_tokens * a.c.hq - 1] = 1.f;
+  CHECK(a.weight_splits >= 1 && a.weight_stride >= a.c.max_len && a.weight_stride % 128 == 0);
+  if (a.weight_splits > 1) {
+    ++weight_parts;
+    a.weight_part[0] = a.weight_part[(int64_t)a.weight_splits * a.c.n_seqs * a.c.hkv * a.weight_stride - 1] = 1.f;
+  }
 }
 void launch_weights_from_logits(const AttendArgs& a, hipStream_t) {
   ++weighings;
@@ -145,7 +150,7 @@ void plans() {
     CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.q, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
     kv_paged_destroy(h);
   }
-  CHECK(attends > 18000 && merges > 1000 && evictions > 1000 && weighings == 6000);
+  CHECK(attends > 18000 && merges > 1000 && evictions > 1000 && weighings == 6000 && weight_parts > 100);
 }
 
 void frequencies() {
