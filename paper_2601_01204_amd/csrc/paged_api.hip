@@ -229,15 +229,21 @@ void plan_workers(const kv_paged* h, AttendArgs& a) {
 }
 
 // Launches of more rows: key ranges per row tile, for the fewest rounds of the workgroups that the chip holds at a time; a workgroup costs
-// about four tiles of 64 keys by itself.
+// about four tiles of 64 keys by itself, and fifty of them as much as one for what the merge reads.  A causal tile has only the ranges that it sees: where
+// the last f of the keys are new, a range that begins at x of them is seen by (1 - x) / f of the tiles (16 heads of 128, 2048 new
+// tokens of 2048: three ranges, 50 us; two, 58; one, 68.  12 heads on two of 128, 27 tokens on 10397: 58 ranges, 28; sixteen, 35).
 void plan_splits(const kv_paged* h, AttendArgs& a) {
   const int64_t keys = reach(a), columns = (int64_t)a.tiles * a.c.hkv;
   const int64_t fit = std::max<int64_t>(1, h->part_rows_cap / std::max<int64_t>(1, columns * a.part_rows));
   const int64_t slots = (h->cfg.head_dim == 128 ? 2ll : 3ll) * h->n_cus, tiles = keys / 64;
+  const double fresh = a.causal && keys >= a.c.max_len ? std::min(1.0, (double)a.c.max_new / a.c.max_len) : 0.0;
   int64_t range = keys;
   double best = 0.0;
-  for (int64_t s = 1; s <= std::min<int64_t>(16, tiles); ++s) {
-    const double cost = (double)((columns * s + slots - 1) / slots) * ((double)((tiles + s - 1) / s) + 4.0) + (s > 1 ? 4.0 : 0.0);
+  for (int64_t s = 1; s <= std::min<int64_t>(64, tiles); ++s) {
+    const int64_t all = std::min(s, (int64_t)((double)s * (1.0 - fresh)) + 1), some = s - all;
+    const double seen = (double)all + (some > 0 ? (double)(some * (some + 1)) / (2.0 * (double)s * fresh) : 0.0);
+    const int64_t blocks = (int64_t)((double)columns * seen);
+    const double cost = (double)((blocks + slots - 1) / slots) * ((double)((tiles + s - 1) / s) + 4.0) + (s > 1 ? 4.0 + 0.02 * (double)blocks : 0.0);
     if (s == 1 || cost < 0.97 * best) {
       best = cost;
       range = (tiles + s - 1) / s * 64;
