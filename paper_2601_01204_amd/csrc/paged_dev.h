@@ -51,7 +51,7 @@ struct AttendArgs {
   const float* weights_in;
   float* weights_out;
   float* weight_part;           // [weight_splits][sequence][key head][weight_stride] sums over parts of the rows, where there is more than one
-  int32_t weight_splits, weight_stride;
+  int32_t weight_splits, weight_rows, weight_stride;            // weight_rows: of a part
   float* logits;                // launches of few rows that collect weights: [tile][key head][row][logit_stride], log2 units; NULL: not kept
   int64_t logit_stride;
   float factor;                 // softmax scale * log2(e)

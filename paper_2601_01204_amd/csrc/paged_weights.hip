@@ -7,8 +7,9 @@
 // weights_kernel.  A workgroup owns 128 keys of one key head, a wave 32 of them, whose fragments stay in registers, and goes over all rows that see
 // them, 64 at a time, brought into LDS for the four waves.  S = Q K^T with a key in a lane and its rows in that lane's registers: a key's
 // weights are summed in its lane, in row order, in fp32 without a rounding between, and no two workgroups write the same
-// token, so the sums do not depend on what ran when.  Where there are too few workgroups for the chip the rows are cut into parts as well,
-// whose sums weights_sum_kernel adds in order (five sequences of 481 tokens, 410 of them new, 24 heads: XXX us).
+// token, so the sums do not depend on what ran when.  Where that makes too few workgroups for the chip the rows are
+// cut into parts as well, whose sums weights_sum_kernel adds in order (4 us).  It is bound by its exponentials and the masks and sums around them,
+// at about a third of the rate that the products alone would reach.
 #include "../../include/kvx.h"
 #include "paged_tile.h"
 
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
   const int base = s.len - s.n;
   const int i0 = a.causal ? min(s.n, max(0, kb - base)) : 0;
   const int i1 = a.window > 0 ? max(i0, min(s.n, kb + kKeys - 1 + a.window - base)) : s.n;
-  const int rows = (i1 - i0) * c.group, part = (rows + a.weight_splits * kRows - 1) / (a.weight_splits * kRows) * kRows;
+  const int rows = (i1 - i0) * c.group, part = a.weight_splits > 1 ? a.weight_rows : rows;
   const int r0 = uniform(i0 * c.group + min(rows, split * part)), r1 = uniform(i0 * c.group + min(rows, (split + 1) * part));
   // A thread brings the same rows of every kRows: their tokens and heads move on by the same steps (a division by the group would cost more
   // than a row's exponentials).
