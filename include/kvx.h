@@ -457,7 +457,8 @@ int kv_paged_append(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
  * seen); NULL: not wanted.  weights_out: device, laid out as pages->weights; for every cached token of every sequence of the
  * call and every key head pages->weights plus the softmax weights the token received, summed over the call's rows and the
  * heads of the group; may be pages->weights itself; other slots are left alone.  NULL: not wanted.  A page may be in
- * several sequences' tables (a shared prefix), but not with weights_out. */
+ * several sequences' tables (a shared prefix), but not with weights_out.  out may be q itself, of q's strides, but not with
+ * weights_out, which may read the queries after out is written; it must not overlap q otherwise. */
 int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* batch, const kv_rows* q, const kv_rows* out,
                     float* lse, int32_t causal, int32_t window, float* weights_out, void* hip_stream);
 

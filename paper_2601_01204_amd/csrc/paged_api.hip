@@ -384,6 +384,10 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   int rc = check_call(h, "kv_paged_attend", pages, batch, &a.c);
   if (rc != KV_OK) return rc;
   if ((rc = check_rows(h, "kv_paged_attend", "q", batch, q, &a.q)) != KV_OK || (rc = check_rows(h, "kv_paged_attend", "out", batch, out, &a.out)) != KV_OK) return rc;
+  if (batch->n_tokens > 0 && q->data == out->data) {
+    if (weights_out) return fail(h, KV_E_INVAL, "kv_paged_attend: out must not be q where weights are collected");
+    if (q->tok_stride != out->tok_stride || q->head_stride != out->head_stride) return fail(h, KV_E_INVAL, "kv_paged_attend: out in the place of q needs its strides");
+  }
   if (window < 0) return fail(h, KV_E_INVAL, "kv_paged_attend: window must be >= 0");
   if (weights_out && !a.c.weights) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out needs pages->weights");
   if ((uintptr_t)lse & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse must be 4-byte aligned");

@@ -75,6 +75,7 @@ class KvPages:
         assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype and k_pages.device == v_pages.device
         assert k_pages.stride() == v_pages.stride() and k_pages.stride(3) == 1, "k_pages and v_pages must have the same strides and contiguous channels"
         assert _is(page_table, "int32") and page_table.dim() == 2 and page_table.stride(1) == 1, "page_table must be int32 [sequences, entries]"
+        assert page_table.shape[0] == 1 or page_table.stride(0) >= page_table.shape[1], "rows of page_table must not overlap"
         slot, head = (2, 1) if heads_first else (1, 2)
         n, self.n_heads, self.page_size, self.head_dim = k_pages.shape[0], k_pages.shape[head], k_pages.shape[slot], k_pages.shape[3]
         for t, name, dt in ((weights, "weights", "float32"), (ids, "ids", "int32")):
@@ -167,8 +168,8 @@ class KvPaged:
             raise AssertionError(f"{name} must have contiguous channels")
         r = self._records[place]
         r.data = t.data_ptr()
-        r.tok_stride = ts if n > 1 or ts > d else d       # (a dimension of one element may carry any stride)
-        r.head_stride = hs if heads > 1 or hs > d else d
+        r.tok_stride = ts if n > 1 else d                 # (a dimension of one element may carry any stride)
+        r.head_stride = hs if heads > 1 else d
         return self._refs[place]
 
     def append(self, pages, batch, k, v, q=None, q_out=None, positions=None, hip_stream: int = 0):

@@ -90,7 +90,7 @@ kv_paged_config config() {
 struct Args {
   kv_pages p{};
   kv_paged_batch b{};
-  kv_rows q{}, k{};
+  kv_rows q{}, k{}, out{};
   explicit Args(const kv_paged_config& c) {
     auto at = [](uintptr_t x) { return (void*)(x << 12); };
     p.k = at(1); p.v = at(2);
@@ -100,6 +100,8 @@ struct Args {
     b.n_seqs = c.max_seqs; b.n_tokens = c.max_tokens; b.max_new = (c.max_tokens + c.max_seqs - 1) / c.max_seqs; b.max_len = c.max_len;
     b.q_start = (int32_t*)at(6); b.kv_lens = (int32_t*)at(7);
     q.data = at(8); q.head_stride = c.head_dim; q.tok_stride = (int64_t)c.head_dim * c.n_q_heads;
+    out = q;
+    out.data = at(12);
     k.data = at(9); k.head_stride = c.head_dim; k.tok_stride = (int64_t)c.head_dim * c.n_kv_heads;
   }
 };
@@ -143,11 +145,11 @@ void plans() {
     kv_pages p = a.p;
     std::vector<float> w(4);
     p.weights = w.data();
-    CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.q, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
+    CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.out, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
     a.b.n_tokens = std::min(c.max_tokens, c.max_seqs);
     a.b.n_seqs = c.max_seqs;
     a.b.max_new = 1;
-    CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.q, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
+    CHECK(kv_paged_attend(h, &p, &a.b, &a.q, &a.out, nullptr, 1, 0, w.data(), nullptr) == KV_OK);
     kv_paged_destroy(h);
   }
   CHECK(attends > 18000 && merges > 1000 && evictions > 1000 && weighings == 6000 && weight_parts > 100);
@@ -194,7 +196,7 @@ void refusals() {
     float *lse = (float*)((uintptr_t)11 << 12), *w = a.p.weights;
     int32_t budget = 300, sinks = 4, recent = 10, window = 0;
     int32_t *ids_out = a.p.ids, *lens_out = (int32_t*)a.b.kv_lens;
-    kv_rows q_out = a.q, v = a.k, out = a.q;
+    kv_rows q_out = a.q, v = a.k, out = a.out;
     const kv_rows *pq = &a.q, *po = &q_out;
     spoil(a, q_out, v, out, pq, po, positions, lse, w, budget, sinks, recent, window, ids_out, lens_out);
     auto is = [&](int rc) {
@@ -254,6 +256,8 @@ void refusals() {
   REFUSED(KV_E_INVAL, kAttend, out.data = nullptr);
   REFUSED(KV_E_INVAL, kAttend, out.tok_stride = 0);
   REFUSED(KV_E_INVAL, kAttend, out.tok_stride = 516);
+  REFUSED(KV_E_INVAL, kAttend, out = a.q);
+  REFUSED(KV_E_INVAL, kAttend, (w = nullptr, out = a.q, out.tok_stride += 8));
   REFUSED(KV_E_INVAL, kAttend, window = -1);
   REFUSED(KV_E_INVAL, kAttend, a.p.weights = nullptr);
   REFUSED(KV_E_INVAL, kAttend, lse = (float*)2);
@@ -280,10 +284,30 @@ void refusals() {
   kv_paged_destroy(h);
 }
 
+// Bounds that the kernels' 32-bit counts hold for.
+void counts() {
+  kv_paged_config c = config();
+  c.n_q_heads = c.n_kv_heads = 256;
+  c.max_seqs = 65536;
+  c.max_len = 1 << 20;
+  c.max_evicted = 1;
+  c.max_tokens = 1;
+  kv_paged* h = make(c);
+  Args a(c);
+  a.b.n_tokens = a.b.max_new = 1;
+  const int64_t before = attends;
+  CHECK(kv_paged_attend(h, &a.p, &a.b, &a.q, &a.out, nullptr, 1, 0, nullptr, nullptr) == KV_E_RANGE);
+  CHECK(attends == before && std::strlen(kv_paged_last_error(h)) > 10);
+  a.b.n_seqs = 1023;
+  CHECK(kv_paged_attend(h, &a.p, &a.b, &a.q, &a.out, nullptr, 1, 0, nullptr, nullptr) == KV_OK);
+  kv_paged_destroy(h);
+}
+
 }  // namespace
 
 int main() {
   plans();
+  counts();
   refusals();
   frequencies();
   int32_t flags = 5;

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2601_01204_amd as kvx
 from oracle import paged_oracle as po
 from tests import paged_util as pu
 
@@ -165,6 +166,27 @@ def test_a_prefix_shared_by_sequences():
     case.pool["table"][2, :2] = case.pool["table"][0, :2]
     case.table.copy_(torch.from_numpy(case.pool["table"]))
     assert run(case) == 0
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens,new", [
+    (5, 5, 64, [700], [612]), (6, 1, 128, [389, 33, 512], [57, 33, 400]), (12, 2, 64, [130, 0, 900], [1, 0, 300]), (16, 1, 64, [17, 260], [17, 33]), (2, 2, 128, [1500], [1500])])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 45), (False, 200)])
+def test_weights_of_many_rows_over_few_keys(hq, hkv, d, lens, new, causal, window):
+    """Few keys and many rows: the rows are weighed in parts, some of which have no row that sees a key."""
+    assert run(pu.Case(lens, new, hq=hq, hkv=hkv, d=d, page=16, seed=d + hq), causal=causal, window=window, weights=True) == 0
+
+
+@pytest.mark.parametrize("new", [1, 9, 200])
+def test_out_in_the_place_of_q(new):
+    case = pu.Case([300, 2000], [new, new], hq=4, hkv=2, d=64, seed=13)
+    h, q = case.handle(), case.rows(4)
+    out = torch.empty_like(q)
+    h.attend(case.pages(), case.batch(), q, out)
+    with pytest.raises(kvx.KvError):
+        h.attend(case.pages(), case.batch(), q, q, weights_out=torch.zeros_like(case.weights))
+    h.attend(case.pages(), case.batch(), q, q)
+    torch.cuda.synchronize()
+    assert torch.equal(q, out)
 
 
 def test_weights_in_place():

@@ -110,6 +110,15 @@ def test_the_binding_refuses_pools(bad):
         _pool(**bad)
 
 
+def test_the_binding_refuses_tables_whose_rows_overlap():
+    one = torch.zeros(1, 4, dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        _pool(page_table=one.expand(3, 4))
+    with pytest.raises(AssertionError):
+        _pool(page_table=torch.zeros(8, dtype=torch.int32).as_strided((3, 4), (2, 1)))
+    assert _pool(page_table=one.expand(3, 4)[:1]).struct.table_stride == 4
+
+
 @pytest.mark.parametrize("bad", [dict(q_start=torch.zeros(2, dtype=torch.int32)), dict(kv_lens=torch.zeros(2)), dict(q_start=torch.zeros(6, dtype=torch.int32)[::2]),
                                  dict(seen=torch.zeros(3, dtype=torch.int32)), dict(seen=torch.zeros(2, dtype=torch.int64))])
 def test_the_binding_refuses_batches(bad):
