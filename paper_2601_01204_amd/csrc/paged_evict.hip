@@ -8,6 +8,9 @@
 // ones receives the i-th of the others.  Sources lie behind the budget and destinations before it, so the moves are free of
 // order.
 //
+// Bound by latency: a chain of dependent loads (lengths, page, ids and weights) and the counting's barriers; 256 caches of 4097 tokens that give up one
+// token each take 14 us, sixteen of 18432 that keep 8192 28 us and their moves (80 MB read and written) 18 us, 4.4 TB/s.
+//
 // move_kernel copies the rows.  A launch that can move few rows only has the selecting workgroup copy them itself.
 #include "../../include/kvx.h"
 #include "paged_types.h"
