@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   const uint64_t slot_bytes = (uint64_t)c.slot_stride << 4, lane_part = (uint64_t)(ld_row & 7) * slot_bytes + 16 * ld_chunk;
   const uint8_t* const kp = c.k + head_offset(c, head);
   const uint8_t* const vp = c.v + head_offset(c, head);
-  u32x4 rk[kLoads], rv[kLoads];                              // rows on their way
+  u32x4 rv[kLoads];                                          // rows of V on their way
   // Where a tile's rows lie, a key a lane: of the tiles of K and of V whose rows are loaded next, with the keys that have no page.
   struct Tile {
     uint64_t at, absent;
@@ -284,6 +284,22 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
     const uint8_t* const q = p + (ld_row - 16 * wave < 8 ? low : high) + lane_part;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) r[i] = *reinterpret_cast<const u32x4*>(q + i * slot_bytes);
+  };
+  // K goes straight to LDS: 64 lanes fill 1 KB, whose pieces they ask for in the order that LDS has them
+  constexpr int kRowsAtOnce = 64 / kLPR;
+  const int dma_row = lane / kLPR;
+  auto bring_k = [&](int buf, const Tile& t) {
+    auto of_row = [&](int row) {
+      return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t.at, row) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(t.at >> 32), row) << 32;
+    };
+    const uint64_t low = of_row(16 * wave), high = of_row(16 * wave + 8);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int row = kRowsAtOnce * i + dma_row, chunk = (lane % kLPR) ^ swizzle<kRB>(row);      // (rows 16 apart swizzle alike)
+      const uint8_t* const q = kp + (row < 8 ? low : high) + (uint64_t)(row & 7) * slot_bytes + 16 * chunk;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)q,
+                                       (__attribute__((address_space(3))) void*)(lds + buf + (16 * wave + kRowsAtOnce * i) * kRB), 16, 0, 0);
+    }
   };
   auto fetch_v = [&]() {
     absent_loaded = tile_v.absent;
@@ -318,23 +334,21 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   f32x16 x, y;                                               // logits of the running unit, then its probabilities; of the next one
   if (k0 < k1) {
     tile_v = tile_at(page_at(k0), k0);
-    fetch(rk, kp, tile_v);
+    bring_k(0, tile_v);
     fetch_v();
     tile_k = tile_at(page_at(k0 + 64), k0 + 64);
-    put(rk, 0);
     put_v(3 * kTile, k0);
     absent = absent_loaded;
     if (k0 + 64 < k1) {
-      fetch(rk, kp, tile_k);
+      bring_k(kTile, tile_k);
       tile_v = tile_k;
       fetch_v();
       tile_v = tile_at(page_at(k0 + 128), k0 + 128);
-      put(rk, kTile);
-      if (k0 + 128 < k1) fetch(rk, kp, tile_v);
       tile_k = tile_at(page_at(k0 + 192), k0 + 192);
       page = page_at(k0 + 256);
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   int kb = 0, kb1 = kTile, kb2 = 2 * kTile, vb = 3 * kTile, vb1 = 4 * kTile;      // buffers: K of the running tile and the next two, V of it and the next
   bool now = live(k0);
@@ -374,15 +388,17 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
           put_v(vb1, u + 64);
           absent_next = absent_loaded;
         }
-        if (u + 128 < k1) fetch_v();
+        if (u + 128 < k1) {
+          bring_k(kb2, tile_v);
+          fetch_v();
+        }
       } else if (u + 128 < k1) {
-        put(rk, kb2);
-        if (u + 192 < k1) fetch(rk, kp, tile_k);
         tile_v = tile_k;
         tile_k = tile_at(page, u + 256);
         page = page_at(u + 320);
       }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     const int kb_free = kb, vb_free = vb;
     kb = kb1;
