@@ -213,11 +213,12 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 // ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
 // Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is d / 4 matrix cycles x 16 (512 for d = 128) and some 290
 // vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
-// before it goes through its exponentials, then the second product of that one.  K is staged two tiles ahead and V one, three tiles of K
-// and two of V in LDS, one barrier a tile; loads are issued a tile before they are stored.
-// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 2790 us, 887 TFLOP/s, matrix cores busy 39 % of the time; with the staging left out 22 % less, with
-// the reads of LDS left out too another 21 %, without the exponentials then 5 %.  Two row blocks a wave, which would halve the reads, do
-// not fit the registers.
+// before it goes through its exponentials, then the second product of that one.  Three tiles of K
+// and two of V lie in LDS, one barrier a tile.  K goes there from memory directly, two tiles ahead; V passes registers, where tiles that not every row
+// sees are cleaned, and is loaded a tile before it is stored.
+// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 2717 us, 911 TFLOP/s, 2836 with K through registers too, the matrix cores busy
+// 39 % of the time then; of 2865 the staging was 22 % and the reads of LDS another 21 %, the exponentials 5 % after that.  Two row blocks a wave,
+// which would halve the reads, do not fit the registers.
 constexpr int kChunkRows = 128;
 
 template <typename T, int D, bool E4M3>
@@ -274,8 +275,12 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   Tile tile_k{0, 0}, tile_v{0, 0};
   uint64_t absent_loaded = 0;                                // of the tile of V in the registers
   int32_t page = 0;                                          // of the tile after tile_k
-  auto page_at = [&](int u) { return u < k1 ? page_of_key(c, b, u + lane, s.len) : 0; };
-  auto tile_at = [&](int32_t pg, int u) { return Tile{slot_offset(c, pg, (u + (lane & 56)) & slot_mask), __ballot(pg < 0)}; };      // (eight rows share it)
+  const int32_t* const entries = c.table + (int64_t)b * c.table_stride;
+  auto page_at = [&](int u) { return u < k1 ? entries[min(u + lane, s.len - 1) >> c.page_shift] : 0; };      // (not looked at before it is needed: that would wait for it)
+  auto tile_at = [&](int32_t entry, int u) {                 // (eight rows share a place)
+    const int32_t pg = (uint32_t)entry < (uint32_t)c.n_pages ? entry : -1;
+    return Tile{slot_offset(c, pg, (u + (lane & 56)) & slot_mask), __ballot(pg < 0)};
+  };
   auto fetch = [&](u32x4 (&r)[kLoads], const uint8_t* p, const Tile& t) {
     auto of_row = [&](int row) {
       return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)t.at, row) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(t.at >> 32), row) << 32;
@@ -301,6 +306,7 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
                                        (__attribute__((address_space(3))) void*)(lds + buf + (16 * wave + kRowsAtOnce * i) * kRB), 16, 0, 0);
     }
   };
+  auto arrived = []() { __builtin_amdgcn_s_waitcnt(0x0F70); };      // vmcnt(0): the barrier does not wait for what is on its way to LDS
   auto fetch_v = [&]() {
     absent_loaded = tile_v.absent;
     if (absent_loaded && threadIdx.x == 0) note_bad_page(c);
@@ -348,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
       page = page_at(k0 + 256);
     }
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  arrived();
   __syncthreads();
   int kb = 0, kb1 = kTile, kb2 = 2 * kTile, vb = 3 * kTile, vb1 = 4 * kTile;      // buffers: K of the running tile and the next two, V of it and the next
   bool now = live(k0);
@@ -398,7 +404,7 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
         page = page_at(u + 320);
       }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    arrived();
     __syncthreads();
     const int kb_free = kb, vb_free = vb;
     kb = kb1;
