@@ -216,9 +216,9 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 // before it goes through its exponentials, then the second product of that one.  Three tiles of K
 // and two of V lie in LDS, one barrier a tile.  K goes there from memory directly, two tiles ahead; V passes registers, where tiles that not every row
 // sees are cleaned, and is loaded a tile before it is stored.
-// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 2717 us, 911 TFLOP/s, 2836 with K through registers too, the matrix cores busy
-// 39 % of the time then; of 2865 the staging was 22 % and the reads of LDS another 21 %, the exponentials 5 % after that.  Two row blocks a wave,
-// which would halve the reads, do not fit the registers.
+// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 2553 us, 969 TFLOP/s, the matrix cores busy 44 % of the time; in turn on a slower card
+// 2717, and 2836 with K through registers too.  Of 2865 there the staging was 22 %, the reads of LDS another 21 %, the exponentials 5 % after that.
+// Two row blocks a wave, which would halve the reads, do not fit the registers.
 constexpr int kChunkRows = 128;
 
 template <typename T, int D, bool E4M3>
