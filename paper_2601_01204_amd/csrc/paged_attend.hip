@@ -211,13 +211,14 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 }
 
 // ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
-// Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is d / 4 matrix cycles x 16 (512 for d = 128) and some 290
-// vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
+// Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is 6 d matrix cycles (768 for d = 128; a third of them the first
+// product) and some 450 vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
 // before it goes through its exponentials, then the second product of that one.  Three tiles of K
 // and two of V lie in LDS, one barrier a tile.  K goes there from memory directly, two tiles ahead; V passes registers, where tiles that not every row
 // sees are cleaned, and is loaded a tile before it is stored.
-// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 2553 us, 969 TFLOP/s, the matrix cores busy 44 % of the time; in turn on a slower card
-// 2717, and 2836 with K through registers too.  Of 2865 there the staging was 22 %, the reads of LDS another 21 %, the exponentials 5 % after that.
+// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 3377 us, 733 TFLOP/s of the formula's operations and 1100 of the matrix
+// cores' own.  Before probabilities were pairs, 2717 us where K through registers took 2836; of 2865 there the staging was 22 %, the reads of LDS
+// another 21 %, the exponentials 5 % after that.
 // Two row blocks a wave, which would halve the reads, do not fit the registers.
 constexpr int kChunkRows = 128;
 
