@@ -167,13 +167,23 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     float* const jo = reinterpret_cast<float*>(lds) + (wave * ROWS + my_row) * D;
     if (my_row < n_rows)
 #pragma unroll
-      for (int i = 0; i < W::kQuads; ++i)
-        *reinterpret_cast<float4*>(jo + ((W::kSpan * i + 4 * j) ^ (4 * (my_row & 7)))) =
-            make_float4(w.quad(i, 0) * mine, w.quad(i, 1) * mine, w.quad(i, 2) * mine, w.quad(i, 3) * mine);
-    if (__ballot(odd))
-      mend_odd_values<T, D, E4M3, 32>(c, b, head, s.len, k0 + 32 * wave, k1, 128, mixed, w.lo, w.hi, W::kSpan, j, [&](int i, int e, float x) {
-        if (my_row < n_rows) jo[(W::kSpan * i + 4 * j + e) ^ (4 * (my_row & 7))] += x;
-      });
+      for (int i = 0; i < W::kQuads; ++i) {
+        const float4 x = make_float4(w.quad(i, 0) * mine, w.quad(i, 1) * mine, w.quad(i, 2) * mine, w.quad(i, 3) * mine);
+        odd |= !(fabsf(x.x) < kInf && fabsf(x.y) < kInf && fabsf(x.z) < kInf && fabsf(x.w) < kInf);
+        *reinterpret_cast<float4*>(jo + ((W::kSpan * i + 4 * j) ^ (4 * (my_row & 7)))) = x;
+      }
+    if (__ballot(odd)) {                                     // (a row whose statistics are NaN stays NaN: they divide it below)
+      float* const mend = my_row < n_rows ? jo : nullptr;
+      auto at = [&](int i, int e) -> float& { return mend[(W::kSpan * i + 4 * j + e) ^ (4 * (my_row & 7))]; };
+      set_odd_values<T, D, E4M3, 32>(
+          c, b, head, s.len, k0 + 32 * wave, k1, 128, w.lo, w.hi, W::kSpan, j,
+          [&](int i, int e) {
+            if (mend) at(i, e) = 0.f;
+          },
+          [&](int i, int e, float x) {
+            if (mend) at(i, e) += x;
+          });
+    }
     __syncthreads();
     const float v_scale = E4M3 && c.v_scale ? c.v_scale[head] : 1.f;
     const int64_t part = ((int64_t)blockIdx.x * 2 + (unit == col.first ? 1 : 0)) * a.part_rows;
@@ -432,6 +442,7 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
       for (int g = 0; g < 4; ++g) {
         const int ch = 32 * cb + 8 * g + 4 * h;
         const float o[4] = {w.o[cb][4 * g] * f, w.o[cb][4 * g + 1] * f, w.o[cb][4 * g + 2] * f, w.o[cb][4 * g + 3] * f};
+        odd |= !(fabsf(o[0]) < kInf && fabsf(o[1]) < kInf && fabsf(o[2]) < kInf && fabsf(o[3]) < kInf);
         if (whole) store_out<T>(a, token, qh, ch, o);
         else *reinterpret_cast<float4*>(a.part_o + part_row * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
       }
@@ -446,20 +457,29 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
   __syncthreads();
   if (odd) *any_odd = 1;
   __syncthreads();
-  if (*any_odd)                                              // (a lane adds to what it has just written)
-    mend_odd_values<T, D, E4M3, 64>(c, b, head, s.len, k0, k1, 64, mixed, w.lo, w.hi, 8, h, [&](int i, int e, float x) {
-      const int ch = 8 * i + 4 * h + e;
-      if (!mine) return;
-      if (whole) {
-        uint16_t* const at = reinterpret_cast<uint16_t*>(a.out.p + (int64_t)token * a.out.tok + (int64_t)qh * a.out.head) + ch;
-        *at = (uint16_t)T::pack(T::low(*at) + x, 0.f);
-      } else {
-        a.part_o[part_row * D + ch] += x;
-      }
-    });
+  if (*any_odd) {                                            // (a lane changes what it has just written; a row whose statistics are NaN stays NaN)
+    const bool mend = mine && w.l < kInf;
+    uint16_t* const o16 = reinterpret_cast<uint16_t*>(a.out.p + (int64_t)token * a.out.tok + (int64_t)qh * a.out.head);
+    set_odd_values<T, D, E4M3, 64>(
+        c, b, head, s.len, k0, k1, 64, w.lo, w.hi, 8, h,
+        [&](int i, int e) {
+          if (!mend) return;
+          if (whole) o16[8 * i + 4 * h + e] = 0;
+          else a.part_o[part_row * D + 8 * i + 4 * h + e] = 0.f;
+        },
+        [&](int i, int e, float x) {
+          if (!mend) return;
+          uint16_t* const at = o16 + 8 * i + 4 * h + e;
+          if (whole) *at = (uint16_t)T::pack(T::low(*at) + x, 0.f);
+          else a.part_o[part_row * D + 8 * i + 4 * h + e] += x;
+        });
+  }
 }
 
 // ---- partial results ------------------------------------------------------------------------------------------------
+// A piece's factor may be zero in fp32, but an infinity that a row sees is the row's whatever its weight.
+__device__ __forceinline__ float weighed(float f, float x) { return fabsf(x) < kInf ? f * x : x; }
+
 // Launches of few rows: WAVES waves join the pieces of one row (token, query head).  A lane has four channels, 256 / D lane groups of a wave
 // take a piece each and the next ones after it, four loads ahead.  One wave is enough for a few pieces; 128 of them took one wave 58 us
 // (128 rows, d = 128, two channels a lane, one piece after the other).
@@ -504,10 +524,10 @@ __global__ __launch_bounds__(256) void merge_kernel(const AttendArgs a, const bo
     const float4 y = *reinterpret_cast<const float4*>(a.part_o + piece(i) * D + ch);
     const float f = __builtin_amdgcn_exp2f(w.x - ref);
     l += f * w.y;
-    x[0] += f * y.x;
-    x[1] += f * y.y;
-    x[2] += f * y.z;
-    x[3] += f * y.w;
+    x[0] += weighed(f, y.x);
+    x[1] += weighed(f, y.y);
+    x[2] += weighed(f, y.z);
+    x[3] += weighed(f, y.w);
   }
 #pragma unroll
   for (int o = kLanes; o < 64; o <<= 1) {
@@ -570,10 +590,10 @@ __global__ __launch_bounds__(256) void merge_tile_kernel(const AttendArgs a, con
     const float4 y = *reinterpret_cast<const float4*>(a.part_o + at * D + ch);
     const float f = __builtin_amdgcn_exp2f(w.x - ref);
     l += f * w.y;
-    x[0] += f * y.x;
-    x[1] += f * y.y;
-    x[2] += f * y.z;
-    x[3] += f * y.w;
+    x[0] += weighed(f, y.x);
+    x[1] += weighed(f, y.y);
+    x[2] += weighed(f, y.z);
+    x[3] += weighed(f, y.w);
   }
   const int row = row0 + r, i_row = row / c.group, token = s.first + i_row, qh = head * c.group + row - i_row * c.group;
   const float f = l == 0.f ? 0.f : (scaled && c.v_scale ? c.v_scale[head] : 1.f) / l;

@@ -364,11 +364,13 @@ __device__ __forceinline__ int32_t page_of_key(const Call& c, int b, int key, in
 }
 __device__ __forceinline__ uint64_t row_offset(const Call& c, int32_t page, int key) { return slot_offset(c, page, key & ((1 << c.page_shift) - 1)); }
 
-// Keys that some rows of a workgroup or wave see and others do not ("mixed" runs of KEYS keys, see mixed() in the kernels): an infinite value
-// or NaN among theirs belongs to the rows that see its key, but a probability of zero times it is NaN in all of them.  So the values of
-// mixed runs come into LDS without such (clean tells whether there were any), and where there were, this adds them in the end to the
-// outputs of the rows that see them, where those lie in memory.  Rare; all lanes of a wave together.  A lane has one row, which sees keys
-// [lo, hi), and of its channels the quads span * q + 4 * part .. + 3; add(q, e, x) adds x to the e-th of quad q.
+// Infinite values and NaN among the values.  A row that sees such a value has it in that channel, whatever its weight (the sum of them, where there are
+// several), and a row that does not see it has no part of it.  The products give neither: a probability that is zero in its type times an infinity is NaN, and
+// so may be a pair's second value times one.  So the values of keys that some rows of a workgroup or wave see and others do not ("mixed" runs, see mixed() in
+// the kernels) come into LDS without such (clean tells whether there were any).  Where there were, or where an output is not finite, set_odd_values
+// looks all values through again and puts the outputs of the rows that see such values right, where those lie in memory.  Rare; all lanes of a
+// wave together, KEYS keys at a time.  A lane has one row, which sees keys [lo, hi), and of its channels the quads span * q + 4 * part .. + 3;
+// clear(q, e) makes the e-th of quad q zero, add(q, e, x) adds x to it.
 template <typename T, bool E4M3>
 __device__ __forceinline__ bool clean(u32x4& r) {
   bool odd = false;
@@ -380,38 +382,55 @@ __device__ __forceinline__ bool clean(u32x4& r) {
   }
   return odd;
 }
-template <typename T, int D, bool E4M3, int KEYS, typename MIXED, typename ADD>
-__device__ __forceinline__ void mend_odd_values(const Call& c, int b, int head, int len, int k0, int k1, int step, MIXED mixed, int lo, int hi, int span, int part,
-                                                ADD add) {
+template <typename T, int D, bool E4M3, int KEYS, typename CLEAR, typename ADD>
+__device__ __forceinline__ void set_odd_values(const Call& c, int b, int head, int len, int k0, int k1, int step, int lo, int hi, int span, int part, CLEAR clear,
+                                               ADD add) {
+  constexpr int kPieces = D * (E4M3 ? 1 : 2) / 16;
   const int lane = threadIdx.x & 63;
-  for (int u = k0; u < k1; u += step) {
-    const int32_t page = page_of_key(c, b, u + lane % KEYS, len);
-    const uint64_t absent = __ballot(page < 0);
-    if (!mixed(u, absent)) continue;
-    for (int i = 0; i < KEYS && u + i < len; ++i) {
-      if ((absent >> i) & 1) continue;
-      const uint8_t* v = c.v + head_offset(c, head) + row_offset(c, __shfl(page, i), u + i);
-      const bool sees = u + i >= lo && u + i < hi;
 #pragma unroll 1
-      for (int q = 0; q * span < D; ++q) {
-        const int ch = q * span + 4 * part;
-        uint32_t w[2];
-        if constexpr (E4M3) {
-          const uint32_t x = *reinterpret_cast<const uint32_t*>(v + ch);
-          w[0] = T::template from_e4m3<false>(x);
-          w[1] = T::template from_e4m3<true>(x);
-        } else {
-          w[0] = *reinterpret_cast<const uint32_t*>(v + 2 * ch);
-          w[1] = *reinterpret_cast<const uint32_t*>(v + 2 * ch + 4);
+  for (int pass = 0; pass < 2; ++pass)
+#pragma unroll 1
+    for (int u = k0; u < k1; u += step) {
+      const int mine = u + lane % KEYS;
+      const int32_t page = page_of_key(c, b, mine, len);
+      bool odd = false;
+      if (page >= 0 && mine < len) {
+        const uint8_t* v = c.v + head_offset(c, head) + row_offset(c, page, mine);
+#pragma unroll 4
+        for (int i = 0; i < kPieces; ++i) {
+          u32x4 w = *reinterpret_cast<const u32x4*>(v + 16 * i);
+          odd |= clean<T, E4M3>(w);
         }
+      }
+      uint64_t keys = __ballot(odd);
+      if (KEYS == 32) keys &= 0xFFFFFFFFull;                 // (two lanes had each key)
+      for (; keys; keys &= keys - 1) {
+        const int i = __ffsll((unsigned long long)keys) - 1;
+        const uint8_t* v = c.v + head_offset(c, head) + row_offset(c, __shfl(page, i), u + i);
+        const bool sees = u + i >= lo && u + i < hi;
+#pragma unroll 1
+        for (int q = 0; q * span < D; ++q) {
+          const int ch = q * span + 4 * part;
+          uint32_t w[2];
+          if constexpr (E4M3) {
+            const uint32_t x = *reinterpret_cast<const uint32_t*>(v + ch);
+            w[0] = T::template from_e4m3<false>(x);
+            w[1] = T::template from_e4m3<true>(x);
+          } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(v + 2 * ch);
+            w[1] = *reinterpret_cast<const uint32_t*>(v + 2 * ch + 4);
+          }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = e & 1 ? T::high(w[e >> 1]) : T::low(w[e >> 1]);
-          if (sees && !(fabsf(x) < kInf)) add(q, e, x);
+          for (int e = 0; e < 4; ++e) {
+            const float x = e & 1 ? T::high(w[e >> 1]) : T::low(w[e >> 1]);
+            if (sees && !(fabsf(x) < kInf)) {
+              if (pass == 0) clear(q, e);
+              else add(q, e, x);
+            }
+          }
         }
       }
     }
-  }
 }
 
 // Which rows a workgroup works on: row tile `t` of sequence `b`; false: none.
