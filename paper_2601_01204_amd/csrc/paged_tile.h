@@ -13,11 +13,13 @@
 // final division.  A row of 8-bit keys is read 16 channels at a time, which serve two matrix instructions: their
 // channels are 32 s + 16 h + 0..7 and 8..15, for the queries too.
 //
-// Softmax.  p = 2^(c s - m) in fp32.  Few rows: m is the largest c s of the row so far, raised only where a key lies more than kGap above
-// it (p stays below 2^kGap, and O and l are rescaled in a rare, wave-uniform branch).  More rows, where vector instructions are dear: m is
+// Softmax.  p = 2^(c s - m) in fp32.  Few rows: m lies kFewLift below the largest c s of the row so far, raised only where a key lies more than kFewGap
+// above that one (O and l are rescaled in a rare, wave-uniform branch).  More rows, where vector instructions are dear: m lies kChunkLift below
 // the largest of the row's first unit, and no maximum is taken after that; only where a unit's sum shows that some p is large (kMost,
-// which fp16 still holds) is the unit formed again and m raised.  The second product takes a probability
+// which fp16 still holds; sixteen equal keys reach half of it) is the unit formed again and m raised.  The second product takes a probability
 // as two 16-bit values, the second what the first one's rounding leaves, so that nothing but the output is rounded to 16 bits.
+// In fp16 an error of 2^-25 remains, half the type's least step: for every key 2^-39 of the row's largest weight (few rows) or 2^-35 (more), which is less
+// than an output's half step of 2^-11 up to 2^28 and 2^24 keys.
 #pragma once
 #include "paged_types.h"
 
@@ -26,7 +28,6 @@
 namespace kvx {
 namespace paged {
 
-constexpr float kGap = 8.0f;
 constexpr float kMost = 32768.0f;
 constexpr float kInf = __builtin_inff();
 
@@ -61,7 +62,7 @@ struct RowBlock {
   typedef Shape<D, E4M3> S;
   u32x4 q[S::kSteps];
   f32x16 o[S::kBlocks];
-  float m, l;                  // in log2 units; l: this lane's half of the keys
+  float m, l;                  // m: the reference, in log2 units; l: this lane's half of the keys
   int lo, hi;                  // keys [lo, hi) are seen by this lane's row
 
   __device__ __forceinline__ void clear() {
@@ -126,14 +127,14 @@ struct RowBlock {
     }
   }
 
-  // m rises to the largest of the unit's logits.
+  // m rises to kChunkLift below the largest of the unit's logits.
   __device__ __forceinline__ void raise(const f32x16& s, float c) {
     float top = fmaxf(s[0], s[1]);
 #pragma unroll
     for (int r = 2; r < 16; ++r) top = fmaxf(top, s[r]);
     {
       const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-      top = c * fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      top = c * fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) - T::kChunkLift;
     }
     const float next = fmaxf(m, top), alpha = next == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - next);
 #pragma unroll
@@ -226,7 +227,7 @@ struct FewRows {
   static constexpr int kBlocks = D / ROWS;             // accumulators of ROWS channels
   u32x4 q[kSteps];
   acc_t o[kBlocks];
-  float m, l;                                          // in log2 units; l: this lane's part of the keys
+  float m, l;                                          // m: the reference, in log2 units; l: this lane's part of the keys
   int lo, hi;                                          // keys [lo, hi) are seen by this lane's row
 
   static __device__ __forceinline__ acc_t mfma(u32x4 a, u32x4 b, acc_t c) {
@@ -319,8 +320,8 @@ struct FewRows {
     float top = fmaxf(x[0], x[1]);
 #pragma unroll
     for (int r = 2; r < kLogits; ++r) top = fmaxf(top, x[r]);
-    top = c * over_row(top, [](float a, float b) { return fmaxf(a, b); });
-    if (__ballot(top > m + kGap)) {                      // (also the first key of a row, whose m is -infinity)
+    top = c * over_row(top, [](float a, float b) { return fmaxf(a, b); }) - T::kFewLift;
+    if (__ballot(top > m + T::kFewGap)) {                    // (also the first key of a row, whose m is -infinity)
       const float next = fmaxf(m, top), alpha = next == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - next);
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)

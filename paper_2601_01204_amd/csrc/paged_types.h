@@ -22,6 +22,9 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 struct Half {
   static constexpr uint32_t kExponent = 0x7C00u;
+  // How softmax places probabilities in the type's range (paged_tile.h): fp16's least step is 2^-24 and its largest value 2^16, so references lie below
+  // the largest logit.
+  static constexpr float kFewLift = 14.0f, kFewGap = 1.0f, kChunkLift = 10.0f;
   // two floats rounded to nearest even, the first in the low half
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
@@ -41,6 +44,7 @@ struct Half {
 };
 struct Brain {
   static constexpr uint32_t kExponent = 0x7F80u;
+  static constexpr float kFewLift = 0.0f, kFewGap = 8.0f, kChunkLift = 0.0f;      // (the range of fp32)
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
   }
