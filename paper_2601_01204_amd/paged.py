@@ -56,6 +56,11 @@ def _library():
     return lib
 
 
+def _current_device():
+    import torch
+    return torch.device("cuda", torch.cuda.current_device())
+
+
 def _is(t, dtype):
     return str(t.dtype) == "torch." + dtype
 
@@ -111,7 +116,8 @@ class KvPagedBatch:
 
 
 class KvPaged:
-    """Owner of one kv_paged handle.  Tensors only supply data_ptr(), strides, types and devices, which are checked against the handle's."""
+    """Owner of one kv_paged handle.  Tensors only supply data_ptr(), strides, types and devices, which are checked against the handle's: its device is
+    the one that was current when it was made."""
 
     def __init__(self, rope_freqs=None, **cfg):
         self.lib = _library()
@@ -136,6 +142,7 @@ class KvPaged:
         if rc != 0:
             raise KvError(rc, self.lib.kv_paged_last_error(None).decode())
         c.rope_freqs = None
+        self.device = _current_device()
         self._hq, self._hkv, self._d = c.n_q_heads, c.n_kv_heads, c.head_dim
         self._append, self._attend, self._evict = self.lib.kv_paged_append, self.lib.kv_paged_attend, self.lib.kv_paged_evict
         self._records = [KvRows() for _ in range(4)]      # of the running call
@@ -151,6 +158,8 @@ class KvPaged:
     def _pages(self, pages, batch):
         if pages.form != self._form:
             raise AssertionError(f"the pool's (heads, channels, page size, type) are {pages.form}, the handle's {self._form}")
+        if pages.device != self.device:
+            raise AssertionError(f"the pool is on {pages.device}, the handle on {self.device}")
         if batch.device != pages.device or batch.n_seqs > pages.n_seqs:
             raise AssertionError("the batch's device or sequences are not the page table's")
 
