@@ -349,6 +349,7 @@ int kv_probe_copy(int64_t bytes, int32_t repeats, void* hip_stream, double* gbyt
  * gives upper bounds.  No call allocates, synchronises or copies; work is enqueued on hip_stream.  A handle owns the
  * rotary frequencies and a workspace (partial results), nothing of the sequences: calls on one handle, replays of
  * captured ones included, must be stream-ordered with each other, and callers that want two at once use two handles.
+ * A handle is not thread-safe: a call enqueues several launches, which another thread's must not come between.
  * The device that was current at kv_paged_init has to be current in every call (KV_E_STATE otherwise) and to hold every
  * device pointer.
  *

@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import threading
 
 from .binding import KV_BF16, KvError, load_library
 
@@ -117,7 +118,7 @@ class KvPagedBatch:
 
 class KvPaged:
     """Owner of one kv_paged handle.  Tensors only supply data_ptr(), strides, types and devices, which are checked against the handle's: its device is
-    the one that was current when it was made."""
+    the one that was current when it was made.  Threads may share a handle: a call's launches are enqueued before another call's."""
 
     def __init__(self, rope_freqs=None, **cfg):
         self.lib = _library()
@@ -145,6 +146,7 @@ class KvPaged:
         self.device = _current_device()
         self._hq, self._hkv, self._d = c.n_q_heads, c.n_kv_heads, c.head_dim
         self._append, self._attend, self._evict = self.lib.kv_paged_append, self.lib.kv_paged_attend, self.lib.kv_paged_evict
+        self._lock = threading.Lock()                     # of the records and the call: the library runs without the interpreter's lock
         self._records = [KvRows() for _ in range(4)]      # of the running call
         self._refs = [C.byref(r) for r in self._records]
         self._type = None                                 # the tensors' dtype, once one has been seen
@@ -184,15 +186,16 @@ class KvPaged:
     def append(self, pages, batch, k, v, q=None, q_out=None, positions=None, hip_stream: int = 0):
         """kv_paged_append.  k, v: [tokens, key heads, d]; q, q_out: [tokens, query heads, d] (q_out may be q); positions: int32 [tokens]."""
         self._pages(pages, batch)
-        rq = self._rows(q, self._hq, batch, "q", 0) if q is not None else None
-        ro = self._rows(q_out, self._hq, batch, "q_out", 1) if q_out is not None else None
         p = None
         if positions is not None:
             assert positions.device == batch.device
             p = _int_array(positions, "positions", batch.n_tokens)
-        rc = self._append(self._h, pages.ref, batch.ref, p, rq, ro, self._rows(k, self._hkv, batch, "k", 2), self._rows(v, self._hkv, batch, "v", 3), hip_stream)
-        if rc:
-            self._check(rc)
+        with self._lock:
+            rq = self._rows(q, self._hq, batch, "q", 0) if q is not None else None
+            ro = self._rows(q_out, self._hq, batch, "q_out", 1) if q_out is not None else None
+            rc = self._append(self._h, pages.ref, batch.ref, p, rq, ro, self._rows(k, self._hkv, batch, "k", 2), self._rows(v, self._hkv, batch, "v", 3), hip_stream)
+            if rc:
+                self._check(rc)
 
     def attend(self, pages, batch, q, out, lse=None, causal=True, window: int = 0, weights_out=None, hip_stream: int = 0):
         """kv_paged_attend.  q, out: [tokens, query heads, d]; lse: fp32 [tokens, query heads]; weights_out: as pages.weights."""
@@ -202,10 +205,12 @@ class KvPaged:
             assert _is(lse, "float32") and lse.shape == (batch.n_tokens, self._hq) and lse.is_contiguous() and lse.device == batch.device, \
                 "lse must be a contiguous float32 [tokens, query heads]"
             p_lse = lse.data_ptr()
-        rc = self._attend(self._h, pages.ref, batch.ref, self._rows(q, self._hq, batch, "q", 0), self._rows(out, self._hq, batch, "out", 1), p_lse,
-                          1 if causal else 0, window, None if weights_out is None else self._meta(pages, weights_out, pages.weights, "weights"), hip_stream)
-        if rc:
-            self._check(rc)
+        p_weights = None if weights_out is None else self._meta(pages, weights_out, pages.weights, "weights")
+        with self._lock:
+            rc = self._attend(self._h, pages.ref, batch.ref, self._rows(q, self._hq, batch, "q", 0), self._rows(out, self._hq, batch, "out", 1), p_lse,
+                              1 if causal else 0, window, p_weights, hip_stream)
+            if rc:
+                self._check(rc)
 
     @staticmethod
     def _meta(pages, t, like, name):
@@ -222,13 +227,15 @@ class KvPaged:
         if lens_out is not None:
             assert lens_out.device == batch.device
             p_lens = _int_array(lens_out, "lens_out", batch.n_seqs)
-        self._check(self._evict(self._h, pages.ref, batch.ref, budget, sinks, recent, self._meta(pages, weights_out, pages.weights, "weights"),
-                                            self._meta(pages, ids_out, pages.ids, "ids"), p_lens, hip_stream))
+        p_weights, p_ids = self._meta(pages, weights_out, pages.weights, "weights"), self._meta(pages, ids_out, pages.ids, "ids")
+        with self._lock:
+            self._check(self._evict(self._h, pages.ref, batch.ref, budget, sinks, recent, p_weights, p_ids, p_lens, hip_stream))
 
     def status(self) -> int:
         """kv_paged_status: KV_PAGED_BAD_PAGE | KV_PAGED_BAD_LENGTH met since the last call (synchronises)."""
         f = C.c_int32(0)
-        self._check(self.lib.kv_paged_status(self._h, C.byref(f)))
+        with self._lock:
+            self._check(self.lib.kv_paged_status(self._h, C.byref(f)))
         return f.value
 
     def close(self):

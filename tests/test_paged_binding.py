@@ -1,5 +1,6 @@
 """The paged cache's binding without a GPU: a stand-in for the library that keeps what it is called with."""
 import ctypes as C
+import threading
 
 import pytest
 import torch
@@ -65,3 +66,31 @@ def test_tensors_that_are_not_on_the_handles_device_are_refused(library, monkeyp
         with pytest.raises(AssertionError, match="cuda:0"):
             call()
     assert library.calls == []
+
+
+def test_two_threads_on_one_handle_do_not_swap_their_rows(library, monkeypatch):
+    """While one thread is in the library, which runs without the interpreter's lock, another one makes its call."""
+    h, pages, batch, _, _ = make(monkeypatch, torch.device("cpu"))
+    qs, outs = ([torch.zeros(3, 4, 64, dtype=torch.bfloat16) for _ in range(2)] for _ in range(2))
+    entered, second_done = threading.Event(), threading.Event()
+
+    def inside(q):
+        if not entered.is_set():
+            entered.set()
+            second_done.wait(1.0)                            # the other call, if nothing holds it back
+
+    library.inside = inside
+    first = threading.Thread(target=h.attend, args=(pages, batch, qs[0], outs[0]))
+    first.start()
+    assert entered.wait(10.0)
+
+    def other():
+        h.attend(pages, batch, qs[1], outs[1])
+        second_done.set()
+
+    second = threading.Thread(target=other)
+    second.start()
+    first.join(10.0)
+    second.join(10.0)
+    seen = [c for c in library.calls if c != "attend"]
+    assert sorted(seen) == sorted((q.data_ptr(), q.data_ptr(), o.data_ptr()) for q, o in zip(qs, outs))
