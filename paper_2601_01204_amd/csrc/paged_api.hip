@@ -137,14 +137,18 @@ int check_rows(kv_paged* h, const char* call, const char* name, const kv_paged_b
   return KV_OK;
 }
 
+int check_device(kv_paged* h, const char* call) {
+  int device = -1;
+  if (hipGetDevice(&device) == hipSuccess && device == h->device) return KV_OK;
+  (void)hipGetLastError();
+  return fail(h, KV_E_STATE, "%s: device %d is current, the handle belongs to device %d", call, device, h->device);
+}
+
 int check_call(kv_paged* h, const char* call, const kv_pages* p, const kv_paged_batch* b, Call* out) {
   if (!p || !b) return fail(h, KV_E_INVAL, "%s: %s is NULL", call, p ? "batch" : "pages");
   const kv_paged_config& c = h->cfg;
-  int device = -1;
-  if (hipGetDevice(&device) != hipSuccess || device != h->device) {
-    (void)hipGetLastError();
-    return fail(h, KV_E_STATE, "%s: device %d is current, the handle belongs to device %d", call, device, h->device);
-  }
+  const int rc = check_device(h, call);
+  if (rc != KV_OK) return rc;
   if (b->n_seqs < 1 || b->n_seqs > c.max_seqs) return fail(h, KV_E_RANGE, "%s: %d sequences, the handle takes 1..%d (max_seqs)", call, b->n_seqs, c.max_seqs);
   if (b->n_tokens < 0 || b->n_tokens > c.max_tokens)
     return fail(h, KV_E_RANGE, "%s: %d new tokens, the handle takes 0..%d (max_tokens)", call, b->n_tokens, c.max_tokens);
@@ -458,6 +462,8 @@ int kv_paged_evict(kv_paged* h, const kv_pages* pages, const kv_paged_batch* bat
 int kv_paged_status(kv_paged* h, int32_t* flags) {
   if (!h) return KV_E_INVAL;
   if (!flags) return fail(h, KV_E_INVAL, "kv_paged_status: flags is NULL");
+  const int rc = check_device(h, "kv_paged_status");      // (another device's work would be waited for)
+  if (rc != KV_OK) return rc;
   const int32_t none = 0;
   if (hipDeviceSynchronize() != hipSuccess || hipMemcpy(flags, h->status, 4, hipMemcpyDeviceToHost) != hipSuccess ||
       hipMemcpy(h->status, &none, 4, hipMemcpyHostToDevice) != hipSuccess)

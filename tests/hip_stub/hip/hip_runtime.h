@@ -37,7 +37,8 @@ inline hipError_t hipMemcpy(void* d, const void* s, size_t n, hipMemcpyKind) { s
 inline hipError_t hipDeviceSynchronize() { return hipSuccess; }
 inline hipError_t hipGetLastError() { return hipSuccess; }
 inline const char* hipGetErrorString(hipError_t) { return "stub"; }
-inline hipError_t hipGetDevice(int* d) { *d = 0; return hipSuccess; }
+inline int stub_device;                // the current one
+inline hipError_t hipGetDevice(int* d) { *d = stub_device; return hipSuccess; }
 inline int stub_cus = 256;             // compute units of the pretended device
 inline bool stub_mean_in_score;        // last scoring launch: whether its blocks form the row mean
 // last attention launch: key ranges, scoring blocks per cache inside it; last step: whether the rewrite takes the merge along and
