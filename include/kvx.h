@@ -356,7 +356,11 @@ int kv_probe_copy(int64_t bytes, int32_t repeats, void* hip_stream, double* gbyt
  * Lengths and page numbers are the device's to read, so no call can refuse them; kernels stay inside what the host gave
  * all the same: a page outside [0, n_pages) holds no tokens (attend sees none of its slots, append drops what belongs
  * there, evict lets its tokens go first), lengths and offsets are cut to [0, max_len], [0, max_new] and [0, n_tokens].
- * kv_paged_status tells whether that happened. */
+ * kv_paged_status tells whether that happened.
+ *
+ * A call that would need a launch of 2^32 threads or more is refused (KV_E_RANGE) before anything is enqueued: kv_paged_evict from
+ * 2^22 sequences x key heads on, kv_paged_attend of few rows from 2^26 new tokens x query heads on; with weights_out from
+ * max_len x key heads = 2^31 on.  (Launches go by the bounds, so generous ones count.) */
 
 enum kv_rope_layout {
   KV_ROPE_HALF = 0,        /* channel i of a head turns with channel i + rotary_dim / 2             */

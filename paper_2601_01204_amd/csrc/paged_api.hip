@@ -197,6 +197,8 @@ int check_call(kv_paged* h, const char* call, const kv_pages* p, const kv_paged_
   return KV_OK;
 }
 
+int too_large(kv_paged* h, const char* call) { return fail(h, KV_E_RANGE, "%s: a launch of this call would need 2^32 threads or more", call); }
+
 int launched(kv_paged* h, const char* call) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? KV_OK : fail(h, KV_E_HIP, "%s: launch failed: %s", call, hipGetErrorString(e));
@@ -377,6 +379,7 @@ int kv_paged_append(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   a.magnitude = h->cfg.rope_magnitude > 0.f ? h->cfg.rope_magnitude : 1.f;
   a.rotary = h->cfg.rotary_dim;
   if (a.c.n_tokens == 0 || a.c.max_new == 0) return KV_OK;
+  if (!append_grid(a, h->cfg.head_dim).fits()) return too_large(h, "kv_paged_append");
   launch_append(a, h->cfg.head_dim, h->cfg.dtype, h->cfg.cache_dtype == KV_E4M3, h->cfg.rope_layout == KV_ROPE_INTERLEAVED, (hipStream_t)hip_stream);
   return launched(h, "kv_paged_append");
 }
@@ -396,7 +399,7 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   if (weights_out && !a.c.weights) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out needs pages->weights");
   if ((uintptr_t)lse & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse must be 4-byte aligned");
   if ((uintptr_t)weights_out & 15) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out must be 16-byte aligned");
-  // units of 128 keys of all sequences and key heads are counted in 32 bits, and are the workgroups that form weights again
+  // units of 128 keys of all sequences and key heads are counted in 32 bits
   if ((int64_t)a.c.n_seqs * ((a.c.max_len + 127) / 128) * a.c.hkv > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: n_seqs * max_len * n_kv_heads is too large");
   hipStream_t st = (hipStream_t)hip_stream;
   const kv_paged_config& c = h->cfg;
@@ -407,13 +410,17 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   a.factor = h->factor;
   a.causal = causal != 0;
   a.window = std::min(window, 1 << 28);      // no sequence is longer
-  if (a.c.n_tokens > 0 && a.c.max_new > 0) {
-    const int64_t rows = (int64_t)a.c.max_new * h->group;
-    const int tile_rows = rows <= kFewRows ? kFewRows : kChunkRows;
+  // the whole plan, then the launches
+  const bool attends = a.c.n_tokens > 0 && a.c.max_new > 0;
+  const int tile_rows = (int64_t)a.c.max_new * h->group <= kFewRows ? kFewRows : kChunkRows;
+  bool joins = false;
+  if (attends) {
     plan_tiles(h, a, tile_rows);
     if (tile_rows == kFewRows) plan_workers(h, a);
     else plan_splits(h, a);
-    if ((int64_t)a.tiles * a.c.hkv * a.splits > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: too many workgroups");
+    joins = a.splits > 1 || a.workers;
+    if ((int64_t)a.tiles * a.c.hkv * a.splits > INT32_MAX || !attend_grid(a).fits() || (joins && !merge_grid(a, c.head_dim).fits()))
+      return too_large(h, "kv_paged_attend");
     // A kept logit is 4 bytes written and 4 read, a key formed again d elements: up to as many rows as make that the same.
     a.logit_stride = align_up(a.c.max_len, 64);
     if (weights_out && tile_rows == kFewRows && 8ll * a.part_rows <= (int64_t)c.head_dim * h->cache_elt &&
@@ -421,14 +428,14 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
       a.logits = h->logits;
     a.part_o = (float*)h->work;
     a.part_ml = (float2*)(h->work + h->part_rows_cap * c.head_dim * 4);
-    launch_attend(a, c.head_dim, c.dtype, e4m3, tile_rows, st);
-    if (a.splits > 1 || a.workers) launch_merge(a, c.head_dim, c.dtype, e4m3, st);
   }
+  if (weights_out && !a.logits) plan_weights(h, a);
+  if (weights_out && !(a.logits ? weights_from_logits_grid(a).fits() : weights_grid(a).fits() && weights_sum_grid(a).fits()))
+    return too_large(h, "kv_paged_attend");
+  if (attends) launch_attend(a, c.head_dim, c.dtype, e4m3, tile_rows, st);
+  if (joins) launch_merge(a, c.head_dim, c.dtype, e4m3, st);
   if (a.logits) launch_weights_from_logits(a, st);
-  if (weights_out && !a.logits) {
-    plan_weights(h, a);
-    launch_weights(a, c.head_dim, c.dtype, e4m3, st);
-  }
+  else if (weights_out) launch_weights(a, c.head_dim, c.dtype, e4m3, st);
   return launched(h, "kv_paged_attend");
 }
 
@@ -455,6 +462,7 @@ int kv_paged_evict(kv_paged* h, const kv_pages* pages, const kv_paged_batch* bat
   a.budget = budget;
   a.sinks = sinks;
   a.recent = recent;
+  if (!select_grid(a).fits()) return too_large(h, "kv_paged_evict");
   launch_evict(a, h->cfg.head_dim, h->cfg.cache_dtype == KV_E4M3, h->arrived, (hipStream_t)hip_stream);
   return launched(h, "kv_paged_evict");
 }

@@ -158,18 +158,15 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(const AppendArgs a,
 }  // namespace
 
 void launch_append(const AppendArgs& a, int d, int dtype, bool e4m3, bool interleaved, hipStream_t st) {
-  const int heads = (a.q.p ? a.c.hq : 0) + 2 * a.c.hkv, turns = (heads * (d >> 4) + 63) / 64;      // of 64 lanes, for a token
+  const dim3 grid((unsigned)append_grid(a, d).x);
   auto go = [&](auto t, auto f8, auto inter) {
-    // all turns (of up to 48 heads of 128 channels) in one wave where that leaves four waves a SIMD on 256 units, one each for fewer tokens:
-    // 6700 tokens of 48 heads 38.5 us with four turns a wave, 36.4 with six
+    // a wave with six turns has all of up to 48 heads of 128 channels: 6700 tokens of 48 heads 38.5 us with four turns a wave, 36.4 with six
     auto with = [&](auto units) {
       constexpr int kUnits = decltype(units)::value;
-      const int slabs = (turns + kUnits - 1) / kUnits;
-      const int64_t jobs = (int64_t)a.c.n_tokens * slabs;
       append_kernel<decltype(t), decltype(f8)::value, decltype(inter)::value, kUnits>
-          <<<dim3((unsigned)((jobs + kWaves - 1) / kWaves)), dim3(64 * kWaves), 0, st>>>(a, d, slabs);
+          <<<grid, dim3(64 * kWaves), 0, st>>>(a, d, (int)parts_of(append_turns(a, d), kUnits));
     };
-    if ((int64_t)a.c.n_tokens * ((turns + 5) / 6) >= 4096) with(std::integral_constant<int, 6>{});
+    if (append_units(a, d) == 6) with(std::integral_constant<int, 6>{});
     else with(std::integral_constant<int, 1>{});
   };
   auto by_layout = [&](auto t, auto f8) {

@@ -620,7 +620,7 @@ void by_type(int d, int dtype, bool e4m3, F&& f) {
 }  // namespace
 
 void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_rows, hipStream_t st) {
-  const dim3 grid((unsigned)(a.workers ? a.workers : (int64_t)a.tiles * a.c.hkv * a.splits));
+  const dim3 grid((unsigned)attend_grid(a).x);
   by_type(d, dtype, e4m3, [&](auto t, auto dd, auto f8) {
     if (tile_rows == 32 && a.part_rows <= 16) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 16><<<grid, dim3(256), 0, st>>>(a);
     else if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 32><<<grid, dim3(256), 0, st>>>(a);
@@ -629,18 +629,13 @@ void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_ro
 }
 
 void launch_merge(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st) {
-  const int64_t rows = (int64_t)a.c.n_tokens * a.c.hq;
+  const dim3 grid((unsigned)merge_grid(a, d).x);
   by_type(d, dtype, false, [&](auto t, auto dd, auto) {
     typedef decltype(t) Type;
     constexpr int kD = decltype(dd)::value;
-    if (a.workers == 0) {
-      const int slices = (a.part_rows + 1024 / kD - 1) / (1024 / kD);
-      merge_tile_kernel<Type, kD><<<dim3((unsigned)((int64_t)a.tiles * a.c.hkv * slices)), dim3(256), 0, st>>>(a, slices, e4m3);
-    } else if (rows * 8 < a.workers) {
-      merge_kernel<Type, kD, 4><<<dim3((unsigned)rows), dim3(256), 0, st>>>(a, e4m3);
-    } else {
-      merge_kernel<Type, kD, 1><<<dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st>>>(a, e4m3);
-    }
+    if (a.workers == 0) merge_tile_kernel<Type, kD><<<grid, dim3(256), 0, st>>>(a, merge_slices(a, kD), e4m3);
+    else if (merge_waves(a) == 4) merge_kernel<Type, kD, 4><<<grid, dim3(256), 0, st>>>(a, e4m3);
+    else merge_kernel<Type, kD, 1><<<grid, dim3(256), 0, st>>>(a, e4m3);
   });
 }
 

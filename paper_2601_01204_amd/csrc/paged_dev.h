@@ -75,6 +75,35 @@ struct EvictArgs {
   int32_t budget, sinks, recent, max_moves;
 };
 
+// ---- workgroups of each launch -------------------------------------------------------
+// The runtime takes fewer than 2^32 threads in a dimension; calls that would need more are refused before anything is enqueued.
+struct Grid {
+  int64_t x = 0, y = 1;
+  int32_t threads = 256;
+  bool fits() const { return x * threads < (1ll << 32) && y <= 65536; }
+};
+constexpr int kSelectThreads = 1024;
+constexpr int kFewMoves = 256;                        // as many rows of a (sequence, key head) are moved by the workgroup that selects
+constexpr int kWeightKeys = 128;                      // keys of a workgroup of the launch that forms weights again
+inline int64_t parts_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
+// All pieces (of 64 lanes, for a token) in one wave where that leaves four waves a SIMD on 256 units, one each for fewer tokens.
+inline int append_turns(const AppendArgs& a, int d) { return (int)parts_of((int64_t)((a.q.p ? a.c.hq : 0) + 2 * a.c.hkv) * (d >> 4), 64); }
+inline int append_units(const AppendArgs& a, int d) { return (int64_t)a.c.n_tokens * parts_of(append_turns(a, d), 6) >= 4096 ? 6 : 1; }
+inline Grid append_grid(const AppendArgs& a, int d) { return Grid{parts_of(a.c.n_tokens * parts_of(append_turns(a, d), append_units(a, d)), 4)}; }
+inline Grid attend_grid(const AttendArgs& a) { return Grid{a.workers ? a.workers : (int64_t)a.tiles * a.c.hkv * a.splits}; }
+// Rows of new tokens that a workgroup of the join takes: of few rows one, or one a wave; of more, 1024 / d of a tile.
+inline int merge_waves(const AttendArgs& a) { return (int64_t)a.c.n_tokens * a.c.hq * 8 < a.workers ? 4 : 1; }
+inline int merge_slices(const AttendArgs& a, int d) { return (int)parts_of(a.part_rows, 1024 / d); }
+inline Grid merge_grid(const AttendArgs& a, int d) {
+  if (a.workers) return Grid{parts_of((int64_t)a.c.n_tokens * a.c.hq * merge_waves(a), 4)};
+  return Grid{(int64_t)a.tiles * a.c.hkv * merge_slices(a, d)};
+}
+// Keys and heads in one dimension, sequences and parts of the rows in the other: max_len is a bound that may be generous.
+inline Grid weights_grid(const AttendArgs& a) { return Grid{parts_of(a.c.max_len, kWeightKeys) * a.c.hkv, (int64_t)a.c.n_seqs * a.weight_splits}; }
+inline Grid weights_sum_grid(const AttendArgs& a) { return Grid{parts_of(a.c.max_len, 256) * a.c.hkv, a.c.n_seqs}; }
+inline Grid weights_from_logits_grid(const AttendArgs& a) { return Grid{parts_of(a.c.max_len, 4 * 256) * a.c.hkv, a.c.n_seqs}; }
+inline Grid select_grid(const EvictArgs& a) { return Grid{(int64_t)a.c.n_seqs * a.c.hkv, 1, kSelectThreads}; }
+
 // ---- launchers (each enqueues on `st`, never synchronises) --------------------------
 // dtype: KV_BF16 or KV_F16; e4m3: the pages hold 8-bit floats.
 void launch_append(const AppendArgs& a, int d, int dtype, bool e4m3, bool interleaved, hipStream_t st);

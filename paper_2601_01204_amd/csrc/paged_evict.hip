@@ -22,9 +22,8 @@ namespace paged {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = kSelectThreads, kWaves = kThreads / 64;
 constexpr uint32_t kProtected = 0xFFFFFFFFu;
-constexpr int kFewMoves = 256;
 constexpr int kFewLeave = 4;                    // tokens that leave by looking for the least: a pass each, where the digits take three longer ones
 
 __device__ __forceinline__ uint32_t key_of(const EvictArgs& a, int32_t id, float w, int seen) {
@@ -420,7 +419,7 @@ void launch_evict(const EvictArgs& a, int d, bool e4m3, int32_t* arrived, hipStr
   const bool here = a.max_moves <= kFewMoves;
   auto go = [&](auto rb) {
     constexpr int kRB = decltype(rb)::value;
-    const dim3 grid((unsigned)jobs), block(kThreads);
+    const dim3 grid((unsigned)select_grid(a).x), block(kThreads);
     if (a.c.max_len <= 4 * kThreads) select_kernel<kRB, 1><<<grid, block, 0, st>>>(a, here, arrived);
     else if (a.c.max_len <= 8 * kThreads) select_kernel<kRB, 2><<<grid, block, 0, st>>>(a, here, arrived);
     else if (a.c.max_len <= 16 * kThreads) select_kernel<kRB, kHold><<<grid, block, 0, st>>>(a, here, arrived);

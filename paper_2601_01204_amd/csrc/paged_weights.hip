@@ -18,7 +18,7 @@ namespace paged {
 
 namespace {
 
-constexpr int kKeys = 128, kRows = 64;
+constexpr int kKeys = kWeightKeys, kRows = 64;
 
 template <typename T, int D, bool E4M3>
 __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
@@ -30,9 +30,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
 
   const Call& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const int key_blocks = (c.max_len + kKeys - 1) / kKeys;
-  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
-  const int block = rest % key_blocks, column = rest / key_blocks, b = column % c.n_seqs, split = column / c.n_seqs;
+  const int head = blockIdx.x % c.hkv, block = blockIdx.x / c.hkv, column = blockIdx.y, b = column % c.n_seqs, split = column / c.n_seqs;
   const Seq s = uniform(sequence(c, b));
   const int kb = block * kKeys;
   if (kb >= s.len) return;
@@ -170,8 +168,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const AttendArgs a) {
 // The sums over the parts of the rows, a key a thread.
 __global__ __launch_bounds__(256) void weights_sum_kernel(const AttendArgs a) {
   const Call& c = a.c;
-  const int key_blocks = (c.max_len + 255) / 256;
-  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv, b = rest / key_blocks, key = (rest - b * key_blocks) * 256 + (int)threadIdx.x;
+  const int head = blockIdx.x % c.hkv, b = blockIdx.y, key = blockIdx.x / c.hkv * 256 + threadIdx.x;
   const Seq s = sequence(c, b);
   if (key >= s.len) return;
   const int32_t page = page_of(c, b, key >> c.page_shift);
@@ -185,13 +182,11 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const AttendArgs a) {
 
 // A thread has four neighbouring keys of one key head.  A row's range of keys (row tiles of decoding see them all but for masks) was
 // written as far as its tile goes; keys that no row of the tile read (in front of a window) have no logits and gain nothing.
-template <int kThreads>
-__global__ __launch_bounds__(kThreads) void weights_from_logits_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256) void weights_from_logits_kernel(const AttendArgs a) {
   const Call& c = a.c;
+  constexpr int kThreads = 256;
   __shared__ float lse[32];
-  const int key_blocks = (c.max_len + 4 * kThreads - 1) / (4 * kThreads);
-  const int head = blockIdx.x % c.hkv, rest = blockIdx.x / c.hkv;
-  const int block = rest % key_blocks, b = rest / key_blocks;
+  const int head = blockIdx.x % c.hkv, block = blockIdx.x / c.hkv, b = blockIdx.y;
   const Seq s = sequence(c, b);
   if (block * 4 * kThreads >= s.len) return;
   const int rows = s.n * c.group;                            // one tile of a sequence's rows
@@ -237,13 +232,13 @@ __global__ __launch_bounds__(kThreads) void weights_from_logits_kernel(const Att
 }  // namespace
 
 void launch_weights_from_logits(const AttendArgs& a, hipStream_t st) {
-  constexpr int kThreads = 256;
-  const dim3 grid((unsigned)((int64_t)((a.c.max_len + 4 * kThreads - 1) / (4 * kThreads)) * a.c.hkv * a.c.n_seqs));
-  weights_from_logits_kernel<kThreads><<<grid, dim3(kThreads), 0, st>>>(a);
+  const Grid g = weights_from_logits_grid(a);
+  weights_from_logits_kernel<<<dim3((unsigned)g.x, (unsigned)g.y), dim3(256), 0, st>>>(a);
 }
 
 void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)((a.c.max_len + kKeys - 1) / kKeys) * a.c.hkv * a.c.n_seqs * a.weight_splits));
+  const Grid all = weights_grid(a), sum = weights_sum_grid(a);
+  const dim3 grid((unsigned)all.x, (unsigned)all.y);
   auto go = [&](auto t, auto dd, auto f8) { weights_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a); };
   auto by_d = [&](auto t, auto f8) {
     if (d == 128) go(t, std::integral_constant<int, 128>{}, f8);
@@ -255,7 +250,7 @@ void launch_weights(const AttendArgs& a, int d, int dtype, bool e4m3, hipStream_
   };
   if (dtype == KV_F16) by_cache(Half{});
   else by_cache(Brain{});
-  if (a.weight_splits > 1) weights_sum_kernel<<<dim3((unsigned)((int64_t)((a.c.max_len + 255) / 256) * a.c.hkv * a.c.n_seqs)), dim3(256), 0, st>>>(a);
+  if (a.weight_splits > 1) weights_sum_kernel<<<dim3((unsigned)sum.x, (unsigned)sum.y), dim3(256), 0, st>>>(a);
 }
 
 }  // namespace paged

@@ -10,7 +10,7 @@ STUB = os.path.join(ROOT, "tests", "hip_stub")
 
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
-@pytest.mark.parametrize("name,says", [("paged_device_check", "paged device checks passed")])
+@pytest.mark.parametrize("name,says", [("paged_device_check", "paged device checks passed"), ("paged_grid_check", "paged grid checks passed")])
 def test_host_program(tmp_path, name, says):
     exe, csrc = str(tmp_path / name), os.path.join(ROOT, "paper_2601_01204_amd", "csrc")
     cmd = ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-static-libasan", "-I", STUB, "-I", csrc,
