@@ -399,8 +399,9 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   if (weights_out && !a.c.weights) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out needs pages->weights");
   if ((uintptr_t)lse & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse must be 4-byte aligned");
   if ((uintptr_t)weights_out & 15) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out must be 16-byte aligned");
-  // units of 128 keys of all sequences and key heads are counted in 32 bits
-  if ((int64_t)a.c.n_seqs * ((a.c.max_len + 127) / 128) * a.c.hkv > INT32_MAX) return fail(h, KV_E_RANGE, "kv_paged_attend: n_seqs * max_len * n_kv_heads is too large");
+  // units of 128 keys of all sequences and key heads are counted in 32 bits, and so is the end of the workers' even shares, up to a unit a worker behind them
+  if (parts_of(a.c.max_len, 128) * a.c.n_seqs * a.c.hkv > INT32_MAX - few_workers(h))
+    return fail(h, KV_E_RANGE, "kv_paged_attend: n_seqs * max_len * n_kv_heads is too large");
   hipStream_t st = (hipStream_t)hip_stream;
   const kv_paged_config& c = h->cfg;
   const bool e4m3 = c.cache_dtype == KV_E4M3;

@@ -116,6 +116,15 @@ int main() {
     Calls c(1024, 256, 128, 1, 1 << 22, 1 << 22, 1 << 22);
     CHECK(c.append(true) == KV_E_RANGE && c.append(false) == KV_OK);
   }
+  // units of 128 keys: workers' shares are rounded up, and where the last one ends is counted in 32 bits too
+  {
+    Calls c(1, 1, 64, 65535, 1, 1, 42966 * 128);
+    c.b.max_len = 32768 * 128;
+    CHECK(c.attend(nullptr) == KV_OK);
+    c.b.n_seqs = 49981;
+    c.b.max_len = 42966 * 128;                        // 2^31 - 2 of them
+    CHECK(c.attend(nullptr) == KV_E_RANGE);
+  }
   // parts of the rows
   {
     Calls c(8, 8, 64, 3, 3000, 1000, 1000);
