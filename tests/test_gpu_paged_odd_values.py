@@ -21,15 +21,15 @@ def put(case, b, j, channels, x):
     rows[:, channels] = raw
 
 
-def check_attend(case, q):
+def check_attend(case, q, window=0):
     h = case.handle()
     out, lse = torch.empty_like(q), torch.empty(case.n_tokens, case.hq, device=case.device)
-    h.attend(case.pages(), case.batch(), q, out, lse=lse)
+    h.attend(case.pages(), case.batch(), q, out, lse=lse, window=window)
     torch.cuda.synchronize()
     h.close()
     scales = [None if x is None else x.numpy() for x in (case.k_scale, case.v_scale)]
     with np.errstate(invalid="ignore"):
-        ref, rl, gained, absolute, reach = po.attend(case.pool, q.float().cpu().numpy(), case.start, case.lens, 1 / math.sqrt(case.d), True, 0, *scales)
+        ref, rl, gained, absolute, reach = po.attend(case.pool, q.float().cpu().numpy(), case.start, case.lens, 1 / math.sqrt(case.d), True, window, *scales)
     finite = np.where(np.isfinite(absolute), absolute, 0.0)
     b_out, b_lse, _ = pu.attend_bounds(case, np.where(np.isfinite(ref), ref, 0.0), finite, rl, gained, reach, True)
     pu.check(out.float().cpu().numpy(), ref, b_out, "out")
@@ -53,6 +53,25 @@ def test_values_that_every_row_sees(dtype, cache, d, length, new, scale):
     assert np.isnan(rows[..., [5, 33]]).all() and np.isfinite(rows[..., [1, 62]]).all()
     if cache != "e4m3":
         assert (rows[..., [0, 20, 63]] == math.inf).all() and (rows[..., 9] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [9, 100])
+@pytest.mark.parametrize("window", [0, 5000])
+def test_values_that_some_rows_see_in_long_caches(dtype, cache, d, new, window):
+    """Among the new tokens and at the window's beginning, where results are joined from partial ones and most weights are zero in fp32."""
+    length, inf = 9000, math.inf if cache != "e4m3" else math.nan
+    case = pu.Case([length], [new], hq=4, hkv=2, d=d, page=16, dtype=dtype, cache=cache, seed=new)
+    first = length - new
+    odd = [(first + new // 2, [3], inf), (first + 5, [3, 8], -inf), (first + 2, [40], math.nan)]
+    if window:                                               # row i sees keys from first + i - window + 1 on
+        odd += [(first - window + 3, [50, 8], inf), (first - window, [51], math.nan), (first - window + 6, [52], -inf)]
+    for j, channels, x in odd:
+        put(case, 0, j, channels, x)
+    ref = check_attend(case, case.rows(4, scale=40.0), window)
+    assert np.isfinite(ref[0, :, [3, 8, 40]] if not window else ref[0, :, [3, 40]]).all() and np.isnan(ref[-1, :, 40]).all()
+    assert np.isfinite(ref[..., [1, 51]]).all()
 
 
 @pytest.mark.parametrize("new", [1, 60])
