@@ -55,8 +55,6 @@ int fail(kv_paged* h, int code, const char* fmt, ...) {
 
 int64_t align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kFewRows = 32, kChunkRows = 128;      // row tiles of the attention kernels
-
 int check_config(const kv_paged_config* c) {
   if (!c) return fail(nullptr, KV_E_INVAL, "kv_paged_init: cfg is NULL");
   if (c->n_kv_heads < 1 || c->n_kv_heads > 256) return fail(nullptr, KV_E_INVAL, "kv_paged_init: n_kv_heads must be in [1, 256]");
@@ -231,7 +229,7 @@ void plan_workers(const kv_paged* h, AttendArgs& a) {
   const int workers = few_workers(h);
   a.splits = 1;
   a.split_keys = (int32_t)keys;
-  a.workers = keys <= 256 || (keys <= 1024 && columns >= 2 * workers) ? 0 : (int32_t)std::min<int64_t>(workers, columns * ((keys + 127) / 128));
+  a.workers = keys <= 256 || (keys <= 1024 && columns >= 2 * workers) ? 0 : (int32_t)std::min<int64_t>(workers, columns * parts_of(keys, kFewKeys));
 }
 
 // Launches of more rows: key ranges per row tile, for the fewest rounds of the workgroups that the chip holds at a time; a workgroup costs
@@ -269,8 +267,8 @@ void plan_splits(const kv_paged* h, AttendArgs& a) {
 // them new: 109 us for the call, 123 at four workgroups, 216 in one part.  The sums lie where attention's partial results were, which the merge in
 // front of this launch has read.
 void plan_weights(const kv_paged* h, AttendArgs& a) {
-  const int64_t stride = align_up(a.c.max_len, 128), blocks = stride / 128 * a.c.hkv * a.c.n_seqs;
-  const int64_t rows = (int64_t)a.c.max_new * h->group, fit = h->part_rows_cap * h->cfg.head_dim / (128 * blocks);
+  const int64_t stride = align_up(a.c.max_len, kWeightKeys), blocks = stride / kWeightKeys * a.c.hkv * a.c.n_seqs;
+  const int64_t rows = (int64_t)a.c.max_new * h->group, fit = h->part_rows_cap * h->cfg.head_dim / (kWeightKeys * blocks);
   const int64_t splits = std::min(std::min<int64_t>(8ll * h->n_cus / blocks, rows / 128), std::min<int64_t>(fit, 32));
   a.weight_splits = (int32_t)std::max<int64_t>(1, splits);
   a.weight_rows = (int32_t)align_up((rows + a.weight_splits - 1) / a.weight_splits, 64);
@@ -399,8 +397,8 @@ int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
   if (weights_out && !a.c.weights) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out needs pages->weights");
   if ((uintptr_t)lse & 3) return fail(h, KV_E_INVAL, "kv_paged_attend: lse must be 4-byte aligned");
   if ((uintptr_t)weights_out & 15) return fail(h, KV_E_INVAL, "kv_paged_attend: weights_out must be 16-byte aligned");
-  // units of 128 keys of all sequences and key heads are counted in 32 bits, and so is the end of the workers' even shares, up to a unit a worker behind them
-  if (parts_of(a.c.max_len, 128) * a.c.n_seqs * a.c.hkv > INT32_MAX - few_workers(h))
+  // units of keys of all sequences and key heads are counted in 32 bits, and so is the end of the workers' even shares, up to a unit a worker behind them
+  if (parts_of(a.c.max_len, kFewKeys) * a.c.n_seqs * a.c.hkv > INT32_MAX - few_workers(h))
     return fail(h, KV_E_RANGE, "kv_paged_attend: n_seqs * max_len * n_kv_heads is too large");
   hipStream_t st = (hipStream_t)hip_stream;
   const kv_paged_config& c = h->cfg;

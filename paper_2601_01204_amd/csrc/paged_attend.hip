@@ -120,9 +120,9 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
     if (u < k1) {
       fetch_page(u);
       fetch_rows(u);
-      fetch_page(u + 128);
+      fetch_page(u + kFewKeys);
     }
-    for (; u < k1; u += 128) {
+    for (; u < k1; u += kFewKeys) {
       const uint32_t absent = absent_next;
       // values behind the end and without a page are zero: a probability of zero times what lies there would not be
       const bool some = mixed(u, absent);
@@ -138,9 +138,9 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // this wave's LDS only: its accesses are carried out in order
       __builtin_amdgcn_wave_barrier();
-      if (u + 128 < k1) {
-        fetch_rows(u + 128);
-        fetch_page(u + 256);
+      if (u + kFewKeys < k1) {
+        fetch_rows(u + kFewKeys);
+        fetch_page(u + 2 * kFewKeys);
       }
       float x[W::kLogits];
       w.logits(lk, lane, x);
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
       float* const mend = my_row < n_rows ? jo : nullptr;
       auto at = [&](int i, int e) -> float& { return mend[(W::kSpan * i + 4 * j + e) ^ (4 * (my_row & 7))]; };
       set_odd_values<T, D, E4M3, 32>(
-          c, b, head, s.len, k0 + 32 * wave, k1, 128, w.lo, w.hi, W::kSpan, j,
+          c, b, head, s.len, k0 + 32 * wave, k1, kFewKeys, w.lo, w.hi, W::kSpan, j,
           [&](int i, int e) {
             if (mend) at(i, e) = 0.f;
           },
@@ -224,13 +224,13 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 // Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is 6 d matrix cycles (768 for d = 128; a third of them the first
 // product) and some 450 vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
 // before it goes through its exponentials, then the second product of that one.  Three tiles of K
-// and two of V lie in LDS, one barrier a tile.  K goes there from memory directly, two tiles ahead; V passes registers, where tiles that not every row
-// sees are cleaned, and is loaded a tile before it is stored.
+// and two of V lie in LDS, one barrier a tile.  K goes there from memory directly; V passes registers, where tiles that not every row sees are
+// cleaned.  Both are asked for in the middle of a tile, for the tile after the next; but the compiler has them arrive before the running tile's last
+// transposing reads of V, which it cannot tell from K's destination, so what they have in fact is the softmax of a unit.
 // Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 3377 us, 733 TFLOP/s of the formula's operations and 1100 of the matrix
 // cores' own.  Before probabilities were pairs, 2717 us where K through registers took 2836; of 2865 there the staging was 22 %, the reads of LDS
 // another 21 %, the exponentials 5 % after that.
 // Two row blocks a wave, which would halve the reads, do not fit the registers.
-constexpr int kChunkRows = 128;
 
 template <typename T, int D, bool E4M3>
 __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a) {
@@ -622,8 +622,8 @@ void by_type(int d, int dtype, bool e4m3, F&& f) {
 void launch_attend(const AttendArgs& a, int d, int dtype, bool e4m3, int tile_rows, hipStream_t st) {
   const dim3 grid((unsigned)attend_grid(a).x);
   by_type(d, dtype, e4m3, [&](auto t, auto dd, auto f8) {
-    if (tile_rows == 32 && a.part_rows <= 16) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 16><<<grid, dim3(256), 0, st>>>(a);
-    else if (tile_rows == 32) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 32><<<grid, dim3(256), 0, st>>>(a);
+    if (tile_rows == kFewRows && a.part_rows <= 16) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 16><<<grid, dim3(256), 0, st>>>(a);
+    else if (tile_rows == kFewRows) attend_few_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value, 32><<<grid, dim3(256), 0, st>>>(a);
     else attend_chunk_kernel<decltype(t), decltype(dd)::value, decltype(f8)::value><<<grid, dim3(256), 0, st>>>(a);
   });
 }

@@ -33,6 +33,9 @@ struct Call {
 
 constexpr int kStatusPage = 1, kStatusLength = 2;
 
+constexpr int kFewRows = 32, kChunkRows = 128;        // row tiles of the two attention kernels
+constexpr int kFewKeys = 128;                         // a unit of keys in launches of few rows
+
 struct AppendArgs {
   Call c;
   Rows q, q_out, k, v;

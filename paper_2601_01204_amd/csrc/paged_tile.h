@@ -485,7 +485,6 @@ __device__ __forceinline__ int split_end(const AttendArgs& a, const Range& r, in
 }
 
 // ---- launches of few rows: a column is a sequence's keys for one key head, a unit kFewKeys of them ----------------------
-constexpr int kFewKeys = 128;
 __device__ __forceinline__ int units_of(const AttendArgs& a, const Seq& s) {
   if (s.n == 0) return 0;
   const Range r = tile_range(a, s, 0, s.n * a.c.group);
