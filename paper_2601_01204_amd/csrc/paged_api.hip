@@ -235,7 +235,7 @@ void plan_workers(const kv_paged* h, AttendArgs& a) {
 // Launches of more rows: key ranges per row tile, for the fewest rounds of the workgroups that the chip holds at a time; a workgroup costs
 // about four tiles of 64 keys by itself, and fifty of them as much as one for what the merge reads.  A causal tile has only the ranges that it sees: where
 // the last f of the keys are new, a range that begins at x of them is seen by (1 - x) / f of the tiles (16 heads of 128, 2048 new
-// tokens of 2048: three ranges, 50 us; two, 58; one, 68.  12 heads on two of 128, 27 tokens on 10397: 58 ranges, 28; sixteen, 35).
+// tokens of 2048: three ranges, 53 us; two, 62; one, 67.  12 heads on two of 128, 27 tokens on 10397: 33 ranges, 27; sixteen, 35; 58, 30).
 void plan_splits(const kv_paged* h, AttendArgs& a) {
   const int64_t keys = reach(a), columns = (int64_t)a.tiles * a.c.hkv;
   const int64_t fit = std::max<int64_t>(1, h->part_rows_cap / std::max<int64_t>(1, columns * a.part_rows));
@@ -264,7 +264,7 @@ void plan_splits(const kv_paged* h, AttendArgs& a) {
 
 // Parts of the rows in the launch that forms weights again: as many as give a compute unit eight workgroups (a key late in a causal call
 // has few rows, and its workgroups end at once), of at least 128 rows.  12 heads on two of 64, three sequences of 2330 tokens, 1985 of
-// them new: 109 us for the call, 123 at four workgroups, 216 in one part.  The sums lie where attention's partial results were, which the merge in
+// them new: 112 us for the call, 120 at four workgroups, 218 at one, 327 in one part.  The sums lie where attention's partial results were, which the merge in
 // front of this launch has read.
 void plan_weights(const kv_paged* h, AttendArgs& a) {
   const int64_t stride = align_up(a.c.max_len, kWeightKeys), blocks = stride / kWeightKeys * a.c.hkv * a.c.n_seqs;

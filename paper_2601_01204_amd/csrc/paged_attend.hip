@@ -30,7 +30,8 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -
 // whatever the sequences' lengths: a worker's share ends inside a column, and merge_kernel joins the pieces.  Against ranges of
 // equal length, several to a slot, us: 64 sequences of up to 8192 tokens 207 -> 186, four of 131072 in 8 bits 215 -> 171 (1.07 GB
 // each: 5.8 and 6.3 TB/s, where a loop that only reads reaches 6.2, and 7.0 past the caches).  128 keys of a wave's products and exponentials take
-// 7 to 14 % of the matrix cores' time: nothing but the loads in flight counts.
+// 7 to 14 % of the matrix cores' time: nothing but the loads in flight counts.  Rows 17 to 32 of d = 128 in 16 bits need more registers than there are (140 bytes a
+// lane go to memory): 32 sequences of 4096, 8 key heads: 101 us at 16 rows a key head, 124 at 32.
 template <typename T, int D, bool E4M3, int ROWS>
 __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) {
   typedef Shape<D, E4M3> S;
@@ -221,15 +222,15 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 }
 
 // ---- more rows: four waves of 32 rows share tiles of 64 keys ------------------------------------------------------
-// Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is 6 d matrix cycles (768 for d = 128; a third of them the first
-// product) and some 450 vector cycles, 128 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while the unit
-// before it goes through its exponentials, then the second product of that one.  Three tiles of K
+// Bound by the matrix cores and the vector units together: a unit (32 keys x 32 rows) is 6 d matrix cycles (768 for d = 128, a third of them the first
+// product) and some 190 vector instructions, 16 of them exponentials.  So the work of a wave is a pipeline of units: the first product of one runs while
+// the unit before it goes through its exponentials, then the second product of that one.  Three tiles of K
 // and two of V lie in LDS, one barrier a tile.  K goes there from memory directly; V passes registers, where tiles that not every row sees are
 // cleaned.  Both are asked for in the middle of a tile, for the tile after the next; but the compiler has them arrive before the running tile's last
 // transposing reads of V, which it cannot tell from K's destination, so what they have in fact is the softmax of a unit.
-// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 3377 us, 733 TFLOP/s of the formula's operations and 1100 of the matrix
-// cores' own.  Before probabilities were pairs, 2717 us where K through registers took 2836; of 2865 there the staging was 22 %, the reads of LDS
-// another 21 %, the exponentials 5 % after that.
+// Two sequences of 20480 tokens, 4096 of them new, 32 heads on 8 of 128: 3.40 ms, 727 TFLOP/s of the formula's operations and 1090 of the matrix
+// cores' own, which are busy 55 % of the time.  Before probabilities were pairs, 2717 us where K through registers took 2836; of 2865 there the
+// staging was 22 %, the reads of LDS another 21 %, the exponentials 5 % after that.
 // Two row blocks a wave, which would halve the reads, do not fit the registers.
 
 template <typename T, int D, bool E4M3>

@@ -113,8 +113,10 @@ int main() {
   }
   // rows of 1536 heads
   {
-    Calls c(1024, 256, 128, 1, 1 << 22, 1 << 22, 1 << 22);
+    Calls c(1024, 256, 128, 1, 1 << 21, 1 << 21, 1 << 21);
     CHECK(c.append(true) == KV_E_RANGE && c.append(false) == KV_OK);
+    c.b.n_tokens = c.b.max_new = (1 << 21) - 1;
+    CHECK(c.append(true) == KV_OK);
   }
   // units of 128 keys: workers' shares are rounded up, and where the last one ends is counted in 32 bits too
   {
