@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256, 2) void attend_few_kernel(const AttendArgs a) 
 #pragma unroll
       for (int i = 0; i < W::kQuads; ++i) {
         const float4 x = make_float4(w.quad(i, 0) * mine, w.quad(i, 1) * mine, w.quad(i, 2) * mine, w.quad(i, 3) * mine);
-        odd |= !(fabsf(x.x) < kInf && fabsf(x.y) < kInf && fabsf(x.z) < kInf && fabsf(x.w) < kInf);
+        odd |= w.l < kInf && !(fabsf(x.x) < kInf && fabsf(x.y) < kInf && fabsf(x.z) < kInf && fabsf(x.w) < kInf);
         *reinterpret_cast<float4*>(jo + ((W::kSpan * i + 4 * j) ^ (4 * (my_row & 7)))) = x;
       }
     if (__ballot(odd)) {                                     // (a row whose statistics are NaN stays NaN: they divide it below)
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void attend_chunk_kernel(const AttendArgs a
       for (int g = 0; g < 4; ++g) {
         const int ch = 32 * cb + 8 * g + 4 * h;
         const float o[4] = {w.o[cb][4 * g] * f, w.o[cb][4 * g + 1] * f, w.o[cb][4 * g + 2] * f, w.o[cb][4 * g + 3] * f};
-        odd |= !(fabsf(o[0]) < kInf && fabsf(o[1]) < kInf && fabsf(o[2]) < kInf && fabsf(o[3]) < kInf);
+        odd |= w.l < kInf && !(fabsf(o[0]) < kInf && fabsf(o[1]) < kInf && fabsf(o[2]) < kInf && fabsf(o[3]) < kInf);
         if (whole) store_out<T>(a, token, qh, ch, o);
         else *reinterpret_cast<float4*>(a.part_o + part_row * D + ch) = make_float4(o[0], o[1], o[2], o[3]);
       }
