@@ -459,10 +459,11 @@ int kv_paged_append(kv_paged* h, const kv_pages* pages, const kv_paged_batch* ba
  * 0 <= j < len, with causal != 0 only j <= p, with window > 0 only j > p - window.  out: softmax of softmax_scale q.k over them times
  * the values, zero where a row sees nothing; keys and values that a row does not see have no part in its result whatever
  * they hold, and an infinite value that it sees (or NaN) is its channel's result whatever its weight.  With dtype KV_F16 a key's
- * softmax weight enters out with an error of up to 2^-39 of the row's largest, 2^-35 in calls of max_new * Hq / Hkv > 32.  lse: device, [n_tokens][Hq] fp32, natural logarithm of the softmax's sum (-infinity where nothing is
- * seen); NULL: not wanted.  weights_out: device, laid out as pages->weights; for every cached token of every sequence of the
- * call and every key head pages->weights plus the softmax weights the token received, summed over the call's rows and the
- * heads of the group; may be pages->weights itself; other slots are left alone.  NULL: not wanted.  A page may be in
+ * softmax weight enters out with an error of up to 2^-39 of the row's largest, 2^-35 in calls of max_new * Hq / Hkv > 32.
+ * lse: device, [n_tokens][Hq] fp32, natural logarithm of the softmax's sum (-infinity where nothing is seen); NULL: not wanted.
+ * weights_out: device, laid out as pages->weights; for every cached token of every sequence of the call and every key head
+ * pages->weights plus the softmax weights the token received, summed over the call's rows and the heads of the group; may be
+ * pages->weights itself; other slots are left alone.  NULL: not wanted.  A page may be in
  * several sequences' tables (a shared prefix), but not with weights_out.  out may be q itself, of q's strides, but not with
  * weights_out, which may read the queries after out is written; it must not overlap q otherwise. */
 int kv_paged_attend(kv_paged* h, const kv_pages* pages, const kv_paged_batch* batch, const kv_rows* q, const kv_rows* out,
